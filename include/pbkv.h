@@ -46,13 +46,13 @@
  *       k_new, v_new  [N][num_kv_heads][head_dim]
  *       kv_pool       [num_pages][2][num_kv_heads][page_size][head_dim]
  *                     (index 0 = K, 1 = V): one page is one contiguous block
- *                     of pbkv_page_bytes() bytes
+ *                     of pbkv_page_bytes() bytes (8-bit pools: see below)
  *       block_table   [batch][max_pages_per_req] int32: physical page of each
  *                     logical page of the request (prefix pages first, then
  *                     the pages the suffix is appended to)
  *   - Supported shapes: page_size 16; head_dim 64 or 128; num_q_heads a
  *     multiple of num_kv_heads with ratio 1, 2, 4, 8 or 16 for PBKV_BF16 and
- *     any ratio for PBKV_F32.  Anything else returns PBKV_ERR_SHAPE; there is
+ *     PBKV_BF16_KV8, any ratio for PBKV_F32.  Anything else returns PBKV_ERR_SHAPE; there is
  *     no slow fallback.
  */
 #ifndef PBKV_H
@@ -73,10 +73,12 @@ typedef enum {
     PBKV_ERR_ALIAS = -5,   /* duplicate destination pages in a swap-in            */
     PBKV_ERR_DEVICE = -6,  /* HIP runtime error, or a pointer of the wrong kind   */
     PBKV_ERR_LIMIT = -7    /* the call needs more descriptor space than the library
-                              can provide at once, or the pool is 1 TiB or more   */
+                              can provide at once, or the pool is 1 TiB (8-bit:
+                              512 GiB) or more                                    */
 } pbkv_status;
 
-typedef enum { PBKV_BF16 = 0, PBKV_F32 = 1 } pbkv_dtype;
+/* PBKV_BF16_KV8: q, k_new, v_new and out are bf16, the pool holds 8-bit rows (see "8-bit pool" below). */
+typedef enum { PBKV_BF16 = 0, PBKV_F32 = 1, PBKV_BF16_KV8 = 2 } pbkv_dtype;
 
 typedef struct {
     int32_t batch;              /* B: requests in this call (0 is a valid no-op)   */
@@ -86,11 +88,26 @@ typedef struct {
     int32_t page_size;          /* P: tokens per page (16)                         */
     int32_t num_pages;          /* pages in kv_pool                                */
     int32_t max_pages_per_req;  /* row length of block_table                       */
-    int32_t dtype;              /* pbkv_dtype of q, k_new, v_new, kv_pool, out     */
+    int32_t dtype;              /* pbkv_dtype of q, k_new, v_new, out, and the pool's form */
 } pbkv_shape;
 
-/* Bytes of one pool page for this shape (2 * H_kv * P * d * element size); 0 if the
- * shape is unsupported. */
+/*
+ * 8-bit pool (PBKV_BF16_KV8).  A row (K or V of one token and KV head) is d e4m3 codes (1 sign, 4 exponent, 3 mantissa bits; no infinities)
+ * and one scale byte b, and stands for the values code * 2^(b - 127).  pbkv_append_kv quantises bf16 rows on their way in:
+ *     e    = the smallest exponent with which the row's largest finite magnitude is at most 448 * 2^e, within [-111, 119];  b = e + 127
+ *     code = x * 2^-e rounded to the nearest e4m3 number, ties to even; above 448 * 2^119 it saturates; infinities and NaN become NaN
+ * so a value is off by at most 2^-4 of itself, or by 2^(e - 10) where it is below 2^(e - 6).  The values are bf16 numbers
+ * without further rounding: attention over the pool computes what it would over a bf16 pool that holds them.  A page is one contiguous
+ * block of pbkv_page_bytes() bytes, which the swaps move as they are:
+ *     codes  [2][num_kv_heads][page_size][head_dim]   (index 0 = K, 1 = V)
+ *     scales [num_kv_heads][page_size][2]             (K, V)
+ *     nothing up to a multiple of 128 bytes           (never written, never read)
+ * Scale bytes have to be in 16 .. 246, as append leaves them, in every slot that a call reads as a token.  In all calls the same
+ * limits hold as for PBKV_BF16, but for the pool's size, which is less than 512 GiB.
+ */
+
+/* Bytes of one pool page for this shape: 2 * H_kv * P * d * element size, or 2 * H_kv * P * (d + 1) rounded up to a multiple of 128
+ * for PBKV_BF16_KV8; 0 if the shape is unsupported. */
 int64_t pbkv_page_bytes(const pbkv_shape *shape);
 
 /*
@@ -107,6 +124,7 @@ int64_t pbkv_page_bytes(const pbkv_shape *shape);
  *   q, k_new, v_new, kv_pool, block_table : device, read only
  *   prefix_lens, new_lens                 : host int32 [batch], read during the call
  *   out                                   : device, written; rows of other calls untouched
+ * With an 8-bit pool the prefix is the values that the pool holds; the suffix, k_new and v_new, is not quantised.
  * bf16: fp32 accumulation, probabilities rounded to bf16 before the PV product, one
  * final rounding to bf16.  f32: fp32 throughout.
  * A call repeated on the same inputs gives the same bits (unless memory for partial results runs out in
@@ -132,8 +150,8 @@ int pbkv_prefix_prefill(const pbkv_shape *shape, const void *q, const void *k_ne
 /*
  * Paged KV append (Sec. 1: the KV-Cache an agent produces is retained for downstream
  * agents).  Suffix token t of request r is copied, for K and V and every KV head, to
- * page block_table[r][(p + t) / P], slot (p + t) % P.  Byte-exact copy; no other pool
- * byte is written.
+ * page block_table[r][(p + t) / P], slot (p + t) % P.  Byte-exact copy, or with an 8-bit pool the row's codes and scale byte; no other
+ * pool byte is written.
  *   k_new, v_new, block_table : device, read only;  kv_pool : device, written
  *   prefix_lens, new_lens     : host int32 [batch]
  * Requests must not share a destination slot (their suffix pages are private).
@@ -141,6 +159,18 @@ int pbkv_prefix_prefill(const pbkv_shape *shape, const void *q, const void *k_ne
 int pbkv_append_kv(const pbkv_shape *shape, const void *k_new, const void *v_new,
                    void *kv_pool, const int32_t *block_table, const int32_t *prefix_lens,
                    const int32_t *new_lens, void *stream);
+
+/*
+ * The way back, for a cache that moves to another pool, form or machine: row t of request r in k and v (packed as k_new and v_new
+ * are) := K and V of token first_tokens[r] + t, t in [0, num_tokens[r]), of every KV head.  Byte-exact copy, or from an 8-bit pool the bf16
+ * numbers that the codes stand for, exactly (appending them to an 8-bit pool again gives values that are the same).
+ *   kv_pool, block_table : device, read only;  k, v : device, [sum of num_tokens][num_kv_heads][head_dim], written
+ *   first_tokens, num_tokens : host int32 [batch]
+ * Errors as for pbkv_append_kv.
+ */
+int pbkv_read_kv(const pbkv_shape *shape, const void *kv_pool, const int32_t *block_table,
+                 const int32_t *first_tokens, const int32_t *num_tokens, void *k, void *v,
+                 void *stream);
 
 /*
  * Host -> pool page swap-in (Sec. 2: HiCache keeps evicted cache in host memory and
@@ -165,7 +195,7 @@ int pbkv_swap_in_pages(const pbkv_shape *shape, const void *host_pages,
  *     out[r][h] = sum_t softmax_t(q[r][h] . k_t / sqrt(d)) v_t   over t in [0, context_lens[r])
  * with k_t, v_t read from kv_pool through block_table[r] (KV head h / (H_q / H_kv)); the row's own
  * token is expected to be in the pool already (append first).  context_lens[r] == 0 gives a zero row.
- *   q, out      : device, [batch][H_q][d], bf16 (other dtypes: PBKV_ERR_DTYPE)
+ *   q, out      : device, [batch][H_q][d], bf16 (PBKV_F32: PBKV_ERR_DTYPE)
  *   kv_pool, block_table : device, read only;   context_lens : host int32 [batch]
  * fp32 accumulation, probabilities kept in fp32, one final rounding to bf16.  The library keeps,
  * per stream, a device scratch buffer for the partial results of context slices (8 MiB on first

@@ -13,7 +13,7 @@ import numpy as np
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libpbkv.so")
 
-PBKV_BF16, PBKV_F32 = 0, 1
+PBKV_BF16, PBKV_F32, PBKV_BF16_KV8 = 0, 1, 2
 STATUS = {0: "PBKV_OK", -1: "PBKV_ERR_NULL", -2: "PBKV_ERR_SHAPE", -3: "PBKV_ERR_DTYPE",
           -4: "PBKV_ERR_RANGE", -5: "PBKV_ERR_ALIAS", -6: "PBKV_ERR_DEVICE", -7: "PBKV_ERR_LIMIT"}
 
@@ -60,6 +60,8 @@ def load():
         lib.pbkv_prefix_prefill.argtypes = [sp, vp, vp, vp, vp, i32p, i32p, i32p, vp, vp]
         lib.pbkv_append_kv.restype = ctypes.c_int
         lib.pbkv_append_kv.argtypes = [sp, vp, vp, vp, i32p, i32p, i32p, vp]
+        lib.pbkv_read_kv.restype = ctypes.c_int
+        lib.pbkv_read_kv.argtypes = [sp, vp, i32p, i32p, i32p, vp, vp, vp]
         lib.pbkv_swap_in_pages.restype = ctypes.c_int
         lib.pbkv_swap_in_pages.argtypes = [sp, vp, i32p, ctypes.c_int32, vp, vp]
         lib.pbkv_paged_decode.restype = ctypes.c_int
@@ -77,7 +79,7 @@ def load():
         lib.pbkv_page_bytes.argtypes = [sp]
         lib.pbkv_last_error.restype = ctypes.c_char_p
         lib.pbkv_version.restype = ctypes.c_char_p
-        for name, kinds in (("prefix_prefill", "spppppiipt"), ("append_kv", "sppppiit"), ("paged_decode", "spppipt"),
+        for name, kinds in (("prefix_prefill", "spppppiipt"), ("append_kv", "sppppiit"), ("read_kv", "sppiippt"), ("paged_decode", "spppipt"),
                             ("paged_decode_static", "spppipt"), ("swap_in_pages", "spiNpt"), ("swap_out_pages", "spiNpt")):
             setattr(lib, "fast_" + name, fast(lib, "pbkv_" + name, kinds, Shape))
         _lib = lib
@@ -139,7 +141,7 @@ def _check(rc):
 
 def make_shape(batch, num_q_heads, num_kv_heads, head_dim, page_size, num_pages,
                max_pages_per_req, dtype):
-    code = {"bf16": PBKV_BF16, "f32": PBKV_F32}.get(dtype, dtype)
+    code = {"bf16": PBKV_BF16, "f32": PBKV_F32, "bf16_kv8": PBKV_BF16_KV8}.get(dtype, dtype)
     return Shape(batch, num_q_heads, num_kv_heads, head_dim, page_size, num_pages,
                  max_pages_per_req, code)
 
@@ -177,6 +179,15 @@ def append_kv(shape, k_new, v_new, kv_pool, block_table, prefix_lens, new_lens, 
     nl, nlp = _host_i32(new_lens)
     _check(load().pbkv_append_kv(ctypes.byref(shape), _ptr(k_new), _ptr(v_new), _ptr(kv_pool),
                                  _ptr(block_table), plp, nlp, _stream(stream)))
+
+
+def read_kv(shape, kv_pool, block_table, first_tokens, num_tokens, k, v, stream=None):
+    rc = load().fast_read_kv(shape, kv_pool, block_table, first_tokens, num_tokens, k, v, stream)
+    if rc is not None:
+        return _check(rc)
+    ft, ftp = _host_i32(first_tokens)
+    nt, ntp = _host_i32(num_tokens)
+    _check(load().pbkv_read_kv(ctypes.byref(shape), _ptr(kv_pool), _ptr(block_table), ftp, ntp, _ptr(k), _ptr(v), _stream(stream)))
 
 
 def swap_in_pages(shape, host_pages, page_ids, kv_pool, stream=None):

@@ -175,18 +175,77 @@ int attn_bf16_tile_tokens(int /*head_dim*/, int group, int waves) {
 // issued at raised wave priority, so that a waiting MFMA of either wave goes before VALU work.
 #define MFMA_PRIO(x) __builtin_amdgcn_s_setprio(x)
 
+#if defined(__HIP_DEVICE_COMPILE__)
+// The tiles of an 8-bit pool: a wave's rows of a tile, one page's and contiguous there, come into registers as codes, 16 (or 8) per lane and load,
+// and go to LDS as the bf16 numbers that they stand for, in the places that the direct loads of bf16 rows fill.  The tile then is what
+// a bf16 pool's would be, and nothing behind it knows the difference.  A code is converted once per work-group, by one instruction for two,
+// its scale with it.  Lanes of rows past the prefix's end read nothing and write zeros.
+template <int D, int NW>
+struct Codes {
+    using Gm = Geom<D, NW>;
+    static constexpr int PER_LANE = Gm::RW * D / 64;             // codes of a K or V tile
+    static constexpr int CB = PER_LANE < 16 ? PER_LANE : 16;     // ... of one load
+    static constexpr int NU = PER_LANE / CB, LPR = D / CB, RPU = 64 / LPR;     // loads, lanes of a row, rows of a load
+    typedef __attribute__((ext_vector_type(CB / 4))) unsigned words;
+    struct Rows { words c[NU]; };
+    struct Scales { unsigned short s[NU]; };                     // of K, then V, of the lane's row
+
+    // slot0: the wave's first slot of the page; bytes: of the page's rows of this head that count
+    static __device__ __forceinline__ void load(Rows &r, const char *rows, int bytes, int slot0, int l) {
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)rows, 0, bytes, 0x00020000);
+#pragma unroll
+        for (int i = 0; i < NU; i++) {
+            const int at = slot0 * D + (i * 64 + l) * CB;
+            if constexpr (CB == 16) r.c[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0);
+            else r.c[i] = __builtin_amdgcn_raw_buffer_load_b64(rsrc, at, 0, 0);
+        }
+    }
+    static __device__ __forceinline__ void load_scales(Scales &s, const char *scales, int bytes, int slot0, int l) {
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)scales, 0, bytes / (D / 2), 0x00020000);
+#pragma unroll
+        for (int i = 0; i < NU; i++) s.s[i] = __builtin_amdgcn_raw_buffer_load_b16(rsrc, (slot0 + i * RPU + l / LPR) * 2, 0, 0);
+    }
+    template <bool V>
+    static __device__ __forceinline__ void store(const Rows &r, const Scales &s, char *buf, int w, int l) {
+#pragma unroll
+        for (int i = 0; i < NU; i++) {
+            const int row = w * Gm::RW + i * RPU + l / LPR;
+            const float scale = __uint_as_float((unsigned)(V ? s.s[i] >> 8 : s.s[i] & 0xff) << 23);
+#pragma unroll
+            for (int h = 0; h < CB / 8; h++) {
+                bf16x8 x;
+#pragma unroll
+                for (int k = 0; k < 2; k++) {
+                    const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[i][2 * h + k], scale, false);
+                    const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[i][2 * h + k], scale, true);
+                    x[4 * k] = lo[0]; x[4 * k + 1] = lo[1]; x[4 * k + 2] = hi[0]; x[4 * k + 3] = hi[1];
+                }
+                const int chunk = (l % LPR) * (CB / 8) + h;
+                *(bf16x8 *)(buf + row * Gm::ROWB + ((chunk ^ (V ? Gm::swz_v(row) : Gm::swz_k(row))) << 4)) = x;
+            }
+        }
+    }
+};
+#endif
+
+// Where a wave's rows of a tile come from: K and V rows, how many bytes of them count, and the scales of an 8-bit pool's page.
+template <bool KV8> struct TileSrc { const char *k, *v; int nrec; };
+template <> struct TileSrc<true> { const char *k, *v; int nrec; const char *scales; };
+
 // PROBE = true builds the gather diagnostic: the work units of a launch without ranges, the same block-table walk, buffer
 // descriptors, loads into LDS and barriers, but instead of the arithmetic every wave XORs the
 // 32-bit words of the valid rows it finds staged, and the work-group stores one word.
 // NAMED = true: the list names the work-groups (AttnParams::units).  (A branch on that costs a launch that has no such list 0.2 us.)
-template <int D, int NW, int KS, bool PROBE, bool NAMED>
+// KV8 = true: the pool holds 8-bit rows.
+template <int D, int NW, int KS, bool PROBE, bool NAMED, bool KV8>
 __global__ __launch_bounds__(64 * NW * KS) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void attn_bf16_kernel(AttnParams p, int G) {
 #if defined(__HIP_DEVICE_COMPILE__)   // the body uses gfx950-only builtins and types; the host pass only needs the stub
     using Gm = Geom<D, NW>;
     constexpr int H = Gm::H;
     constexpr int ROWB = Gm::ROWB;
-    static_assert(KS == 1 || (KS == 2 && NW == 4 && !PROBE), "the shapes that are launched");
+    constexpr int POOLB = KV8 ? D : ROWB;                  // bytes per K/V row of the pool
+    static_assert((KS == 1 || (KS == 2 && NW == 4 && !PROBE)) && !(PROBE && KV8), "the shapes that are launched");
 
     // four separate arrays: the direct-to-LDS loads of one buffer provably do not alias
     // the operand reads of the others
@@ -261,11 +320,12 @@ void attn_bf16_kernel(AttnParams p, int G) {
     // base, or the suffix row base; size = the valid part, so lanes of rows past the prefix
     // end / past the last visible token are out of range and read nothing) plus per-lane
     // byte offsets that never change.  Tiles are asked for in ascending order.
-    struct Src { const char *k, *v; int nrec; };
+    using Src = TileSrc<KV8>;
     const int row_pitch = p.Hkv * ROWB;                    // bytes between suffix tokens
-    const int64_t page_bytes = 2 * (int64_t)p.Hkv * 16 * ROWB;
-    const int64_t v_in_page = (int64_t)p.Hkv * 16 * ROWB;   // V rows follow the K rows of all heads
-    const char *pool_k = (const char *)p.kv_pool + (int64_t)kvh * 16 * ROWB;   // K rows of this head in page 0
+    const int64_t page_bytes = KV8 ? kv8_page_bytes(p.Hkv, D) : 2 * (int64_t)p.Hkv * 16 * ROWB;
+    const int64_t v_in_page = (int64_t)p.Hkv * 16 * POOLB;  // V rows follow the K rows of all heads
+    const char *pool_k = (const char *)p.kv_pool + (int64_t)kvh * 16 * POOLB;  // K rows of this head in page 0
+    const char *pool_s = (const char *)p.kv_pool + kv8_codes_bytes(p.Hkv, D) + kvh * 32;
     const char *kn_h = (const char *)p.k_new + (int64_t)kvh * ROWB;
     const char *vn_h = (const char *)p.v_new + (int64_t)kvh * ROWB;
     auto tile_src = [&](int t) {
@@ -280,7 +340,8 @@ void attn_bf16_kernel(AttnParams p, int G) {
             const int rows = t < TP - 1 ? 16 : max(td.prefix_len - (t * PPT + pw) * 16, 0);
             s.k = pool_k + pg * page_bytes;
             s.v = s.k + v_in_page;
-            s.nrec = rows * ROWB;
+            s.nrec = rows * POOLB;
+            if constexpr (KV8) s.scales = pool_s + pg * page_bytes;
             asm volatile("; source: prefix page");
         } else {
             const int s0 = (t - TP) * BN + w * Gm::RW;         // first suffix token of this wave's rows
@@ -326,6 +387,28 @@ void attn_bf16_kernel(AttnParams p, int G) {
 #pragma unroll
         for (int i = 0; i < Gm::NI; i++) o.v[i] = t < TP ? vv_p[i] : vv_s[i];
         return o; };
+
+    // An 8-bit pool: the rows of K tile t and of V tile t - 1, and the scales of tile t, whose V rows are the next tile's turn; prefix rows into
+    // registers, and from there to LDS when the step's arithmetic has been issued, suffix rows straight to LDS.
+    using Cd = Codes<D, NW>;
+    [[maybe_unused]] typename Cd::Rows codes_k, codes_v;
+    [[maybe_unused]] typename Cd::Scales scales_k, scales_v;
+    auto fetch_codes = [&](const auto &k, const auto &v, int t, bool with_v, char *kbuf, char *vbuf) __attribute__((always_inline)) {
+        if (t < TP) {
+            Cd::load(codes_k, k.k, k.nrec, slot0, l);
+            Cd::load_scales(scales_k, k.scales, k.nrec, slot0, l);
+        } else {
+            issue_loads(k.k, k.nrec, kbuf, offs_k(t));
+        }
+        if (!with_v) return;
+        if (t - 1 < TP) Cd::load(codes_v, v.v, v.nrec, slot0, l);
+        else issue_loads(v.v, v.nrec, vbuf, offs_v(t - 1));
+    };
+    auto store_codes = [&](int t, bool with_v, char *kbuf, char *vbuf) __attribute__((always_inline)) {
+        if (t < TP) Cd::template store<false>(codes_k, scales_k, kbuf, w, l);
+        if (with_v && t - 1 < TP) Cd::template store<true>(codes_v, scales_v, vbuf, w, l);
+        scales_v = scales_k;
+    };
 
     // ---- running state --------------------------------------------------------------------
     f32x16 O[Gm::DB];
@@ -385,10 +468,11 @@ void attn_bf16_kernel(AttnParams p, int G) {
     };
 
     // ---- prologue: K(0) into LDS (a group without tiles takes part in the barriers only) --------
-    Src prev{nullptr, nullptr, 0};
+    Src prev{};
     if (KS == 1 || kt0 < kt1) {
         prev = tile_src(kt0);
-        issue_loads(prev.k, prev.nrec, sK0, offs_k(kt0));
+        if constexpr (KV8) fetch_codes(prev, prev, kt0, false, sK0, nullptr);
+        else issue_loads(prev.k, prev.nrec, sK0, offs_k(kt0));
     }
     __builtin_amdgcn_sched_barrier(0);
     // ---- Q^T operands, pre-scaled: lane (li, lh) holds c * Q[row li][16*dc + 8*lh .. +7] ----
@@ -438,6 +522,9 @@ void attn_bf16_kernel(AttnParams p, int G) {
     for (int i = 0; i < Gm::NI; i++) {
         *(uint4 *)(sV0 + (w * Gm::NI + i) * 1024 + l * 16) = make_uint4(0, 0, 0, 0);
         *(uint4 *)(sV1 + (w * Gm::NI + i) * 1024 + l * 16) = make_uint4(0, 0, 0, 0);
+    }
+    if constexpr (KV8) {
+        if (KS == 1 || kt0 < kt1) store_codes(kt0, false, sK0, nullptr);
     }
     __syncthreads();
 
@@ -557,6 +644,7 @@ void attn_bf16_kernel(AttnParams p, int G) {
         const auto rsrc_v = __builtin_amdgcn_make_buffer_rsrc((void *)prev.v, 0, prev.nrec, RSRC_FLAGS);
         lds_void *dst_k = (lds_void *)(knext + w * Gm::RW * ROWB);
         lds_void *dst_v = (lds_void *)(vcur + w * Gm::RW * ROWB);
+        if constexpr (KV8) fetch_codes(next, prev, j + 1, true, knext, vcur);
         prev = next;
 
         // operand stream: entry m feeds MFMA m of the step
@@ -595,7 +683,7 @@ void attn_bf16_kernel(AttnParams p, int G) {
                 MFMA_PRIO(0);
                 // all tile loads of the step go out in its first half iteration, K and V rows
                 // alternating, one every LD_SP MFMAs: they have the rest of the step to land
-                if constexpr (i == 0 && s2 % LD_SP == 0) {
+                if constexpr (!KV8 && i == 0 && s2 % LD_SP == 0) {
                     constexpr int q = s2 / LD_SP, li2 = q / 2;
                     if constexpr (q % 2 == 0) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_k, dst_k, 16, ok.v[li2], 0, li2 * 1024, 0);
                     else __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_v, dst_v, 16, ov.v[li2], 0, li2 * 1024, 0);
@@ -608,7 +696,7 @@ void attn_bf16_kernel(AttnParams p, int G) {
                 constexpr int s2 = decltype(sc)::value, m = m0 + s2;
                 if constexpr (m == 0) __builtin_amdgcn_sched_group_barrier(SG_DSRD, PF, 0);
                 __builtin_amdgcn_sched_group_barrier(SG_MFMA, 1, 0);
-                if constexpr (i == 0 && s2 % LD_SP == 0) __builtin_amdgcn_sched_group_barrier(SG_VMRD, 1, 0);
+                if constexpr (!KV8 && i == 0 && s2 % LD_SP == 0) __builtin_amdgcn_sched_group_barrier(SG_VMRD, 1, 0);
                 __builtin_amdgcn_sched_group_barrier(SG_VALU, 16 / H, 0);
                 if constexpr (m + PF < NM) __builtin_amdgcn_sched_group_barrier(SG_DSRD, ((m + PF) / H) & 1 ? 2 : 1, 0);
             }, std::make_integer_sequence<int, H>{});
@@ -657,6 +745,7 @@ void attn_bf16_kernel(AttnParams p, int G) {
         };
         iteration(IntC<0>{}, T1, T0, P1, P0);             // block 0 is redone before its PV product
         iteration(IntC<1>{}, T0, T1, P0, P1);
+        if constexpr (KV8) store_codes(j + 1, true, knext, vcur);
         __builtin_amdgcn_s_waitcnt(0x0F70);               // vmcnt(0): K(j+1), V(j) are in LDS
         __syncthreads();                                  // ... and every wave is done with K(j), V(j-1)
     };
@@ -664,8 +753,12 @@ void attn_bf16_kernel(AttnParams p, int G) {
     // moves the reference to block 0's row maximum before anything is exponentiated); K(1), V(0) fetched
     if (KS == 1 || kt0 < kt1) {
         const Src next = tile_src(kt0 + 1);
-        issue_loads(next.k, next.nrec, sK1, offs_k(kt0 + 1));
-        issue_loads(prev.v, prev.nrec, sV0, offs_v(kt0));
+        if constexpr (KV8) {
+            fetch_codes(next, prev, kt0 + 1, true, sK1, sV0);
+        } else {
+            issue_loads(next.k, next.nrec, sK1, offs_k(kt0 + 1));
+            issue_loads(prev.v, prev.nrec, sV0, offs_v(kt0));
+        }
         prev = next;
     }
     if (active && (KS == 1 || kt0 < kt1)) {
@@ -677,6 +770,7 @@ void attn_bf16_kernel(AttnParams p, int G) {
             if (needs_mask(kt0, 0)) mask_block(T0, kt0, 0);
             if (needs_mask(kt0, 1)) mask_block(T1, kt0, 1);
         }
+        if constexpr (KV8) store_codes(kt0 + 1, true, sK1, sV0);
         __builtin_amdgcn_s_waitcnt(0x0F70);
         __syncthreads();
         // full steps kt0 + 1 .. kt1 - 1, in pairs so that the LDS buffers are compile-time constants
@@ -686,13 +780,21 @@ void attn_bf16_kernel(AttnParams p, int G) {
         }
     } else {
         // a wave without rows fetches its part of the tiles for the others
+        if constexpr (KV8) {
+            if (KS == 1 || kt0 < kt1) store_codes(kt0 + 1, true, sK1, sV0);
+        }
         __builtin_amdgcn_s_waitcnt(0x0F70);
         __syncthreads();
         for (int j = kt0 + 1; j < kt1; j++) {
             const Src next = tile_src(j + 1);
             const bool odd = (j - kt0) & 1;
-            issue_loads(next.k, next.nrec, odd ? sK0 : sK1, offs_k(j + 1));
-            issue_loads(prev.v, prev.nrec, odd ? sV1 : sV0, offs_v(j));
+            if constexpr (KV8) {
+                fetch_codes(next, prev, j + 1, true, odd ? sK0 : sK1, odd ? sV1 : sV0);
+                store_codes(j + 1, true, odd ? sK0 : sK1, odd ? sV1 : sV0);
+            } else {
+                issue_loads(next.k, next.nrec, odd ? sK0 : sK1, offs_k(j + 1));
+                issue_loads(prev.v, prev.nrec, odd ? sV1 : sV0, offs_v(j));
+            }
             prev = next;
             __builtin_amdgcn_s_waitcnt(0x0F70);
             __syncthreads();
@@ -872,6 +974,13 @@ static __device__ __forceinline__ void mfma_s_first(f32x16 &d, const i32x4 &a, c
 static __device__ __forceinline__ void mfma_s_acc(f32x16 &d, const i32x4 &a, const i32x4 &b) {
     asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "v"(b));
 }
+// the same with b in accumulation registers
+static __device__ __forceinline__ void mfma_s_first_q(f32x16 &d, const i32x4 &a, const i32x4 &b, const f32x16 &c) {
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %3" : "=&v"(d) : "v"(a), "a"(b), "v"(c));
+}
+static __device__ __forceinline__ void mfma_s_acc_q(f32x16 &d, const i32x4 &a, const i32x4 &b) {
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "a"(b));
+}
 // d += a b, outputs: accumulator in accumulation registers, operands in vector registers
 static __device__ __forceinline__ void mfma_o_acc(f32x16 &d, const i32x4 &a, const i32x4 &b) {
     asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(d) : "v"(a), "v"(b));
@@ -881,7 +990,7 @@ static __device__ __forceinline__ void mfma_o_acc(f32x16 &d, const i32x4 &a, con
 #define SETTLE_A2(x, y) asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 3" : "+a"(x), "+a"(y))
 #endif
 
-template <int D, bool NAMED>
+template <int D, bool NAMED, bool KV8>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1)))
 void attn_bf16_w64_kernel(AttnParams p, int G) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -890,6 +999,7 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
     constexpr int H = Gm::H;
     constexpr int NT = 64 * NW;
     constexpr int ROWB = Gm::ROWB;
+    constexpr int POOLB = KV8 ? D : ROWB;                  // bytes per K/V row of the pool
     constexpr int PFW = 3;                                 // LDS operand prefetch distance, in operand fetches (PFW + 1 divides 4H)
 
     __shared__ __attribute__((aligned(1024))) char sK0[Gm::TILEB];
@@ -942,6 +1052,24 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
         }
     }
 
+    // An 8-bit pool's codes take the vector registers that Q has else; Q's place are accumulation registers then, whose values the
+    // matrix instructions take as they stand.  (Left to the compiler, which moved them to vector registers right before the instruction that
+    // reads them: one cycle too late for an assembly statement, and wrong results.)
+    if constexpr (KV8) {
+#pragma unroll
+        for (int s = 0; s < 2; s++)
+#pragma unroll
+            for (int dc = 0; dc < Gm::DC; dc++) asm volatile("" : "+a"(qreg[s][dc]));
+    }
+    auto s_first = [](f32x16 &d, const i32x4 &a, const i32x4 &b, const f32x16 &c) __attribute__((always_inline)) {
+        if constexpr (KV8) mfma_s_first_q(d, a, b, c);
+        else mfma_s_first(d, a, b, c);
+    };
+    auto s_acc = [](f32x16 &d, const i32x4 &a, const i32x4 &b) __attribute__((always_inline)) {
+        if constexpr (KV8) mfma_s_acc_q(d, a, b);
+        else mfma_s_acc(d, a, b);
+    };
+
     // ---- tile sources (as in the kernel above; a wave's 16 rows of a tile are one page) ----
     constexpr int PPT = BN / 16;
     const int pw = (w * Gm::RW) >> 4;
@@ -950,11 +1078,12 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
     const int n_prefix_pages = (td.prefix_len + 15) >> 4;
     // A wave alone on its SIMD pays for every scalar instruction, so the page ids are held as page
     // offsets in units of 256 bytes (a page is a multiple of that, and a pool of less than 1 TiB
-    // keeps them in 32 bits; the host checks it): a tile's K address is one lane read, one shift and
+    // keeps them in 32 bits; the host checks it; an 8-bit page is one of 128, its pool less than half as large): a tile's K address is one lane read, one shift and
     // one 64-bit add.
+    constexpr int UNIT = KV8 ? 7 : 8;
     const int row_pitch = p.Hkv * ROWB;
-    const int64_t page_bytes = 2 * (int64_t)p.Hkv * 16 * ROWB;
-    const unsigned page_units = (unsigned)(page_bytes >> 8);
+    const int64_t page_bytes = KV8 ? kv8_page_bytes(p.Hkv, D) : 2 * (int64_t)p.Hkv * 16 * ROWB;
+    const unsigned page_units = (unsigned)(page_bytes >> UNIT);
     auto load_id_block = [&](int blk) {
         const int lp = blk * 64 + l;
         int pg = lp < n_prefix_pages ? bt[lp] : 0;
@@ -962,13 +1091,14 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
         return (int)((unsigned)pg * page_units);
     };
     int ids_cur = load_id_block(0), ids_next = load_id_block(1);
-    struct Src { const char *k, *v; int nrec; };
-    const int64_t v_in_page = (int64_t)p.Hkv * 16 * ROWB;
-    const char *pool_k = (const char *)p.kv_pool + (int64_t)kvh * 16 * ROWB;
+    using Src = TileSrc<KV8>;
+    const int64_t v_in_page = (int64_t)p.Hkv * 16 * POOLB;
+    const char *pool_k = (const char *)p.kv_pool + (int64_t)kvh * 16 * POOLB;
+    const char *pool_s = (const char *)p.kv_pool + kv8_codes_bytes(p.Hkv, D) + kvh * 32;
     const char *kn_h = (const char *)p.k_new + (int64_t)kvh * ROWB;
     const char *vn_h = (const char *)p.v_new + (int64_t)kvh * ROWB;
     // rows of this wave's page of the last prefix tile (the only one that can be partly filled or unused)
-    const int last_nrec = min(max(td.prefix_len - ((TP - 1) * PPT + pw) * 16, 0), 16) * ROWB;
+    const int last_nrec = min(max(td.prefix_len - ((TP - 1) * PPT + pw) * 16, 0), 16) * POOLB;
     auto tile_src = [&](int t) {
         Src s;
         if (t < TP) {
@@ -977,9 +1107,10 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
                 ids_next = load_id_block((t >> 4) + 1);
             }
             const unsigned units = (unsigned)__builtin_amdgcn_readlane(ids_cur, (t & 15) * PPT + pw);
-            s.k = pool_k + ((uint64_t)units << 8);
+            s.k = pool_k + ((uint64_t)units << UNIT);
             s.v = s.k + v_in_page;
-            s.nrec = t < TP - 1 ? 16 * ROWB : last_nrec;
+            s.nrec = t < TP - 1 ? 16 * POOLB : last_nrec;
+            if constexpr (KV8) s.scales = pool_s + ((uint64_t)units << UNIT);
         } else {
             const int s0 = (t - TP) * BN + w * Gm::RW;
             const int srows = min(tok_end - s0, Gm::RW);
@@ -1020,6 +1151,27 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
 #pragma unroll
         for (int i = 0; i < Gm::NI; i++) o.v[i] = t < TP ? vv_p[i] : vv_s[i];
         return o; };
+
+    // (as in the kernel above)
+    using Cd = Codes<D, NW>;
+    [[maybe_unused]] typename Cd::Rows codes_k, codes_v;
+    [[maybe_unused]] typename Cd::Scales scales_k, scales_v;
+    auto fetch_codes = [&](const auto &k, const auto &v, int t, bool with_v, char *kbuf, char *vbuf) __attribute__((always_inline)) {
+        if (t < TP) {
+            Cd::load(codes_k, k.k, k.nrec, slot0, l);
+            Cd::load_scales(scales_k, k.scales, k.nrec, slot0, l);
+        } else {
+            issue_loads(k.k, k.nrec, kbuf, offs_k(t));
+        }
+        if (!with_v) return;
+        if (t - 1 < TP) Cd::load(codes_v, v.v, v.nrec, slot0, l);
+        else issue_loads(v.v, v.nrec, vbuf, offs_v(t - 1));
+    };
+    auto store_codes = [&](int t, bool with_v, char *kbuf, char *vbuf) __attribute__((always_inline)) {
+        if (t < TP) Cd::template store<false>(codes_k, scales_k, kbuf, w, l);
+        if (with_v && t - 1 < TP) Cd::template store<true>(codes_v, scales_v, vbuf, w, l);
+        scales_v = scales_k;
+    };
 
     // ---- running state of the two sub-tiles ----
     f32x16 O[2][Gm::DB];
@@ -1071,7 +1223,12 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
 
     // ---- prologue ----
     Src prev = tile_src(0);
-    issue_loads(prev.k, prev.nrec, sK0, offs_k(0));
+    if constexpr (KV8) {
+        fetch_codes(prev, prev, 0, false, sK0, nullptr);
+        store_codes(0, false, sK0, nullptr);
+    } else {
+        issue_loads(prev.k, prev.nrec, sK0, offs_k(0));
+    }
     for (int i = tid; i < Gm::TILEB / 16; i += NT) {
         *(uint4 *)(sV0 + i * 16) = make_uint4(0, 0, 0, 0);
         *(uint4 *)(sV1 + i * 16) = make_uint4(0, 0, 0, 0);
@@ -1192,6 +1349,7 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
         const auto rsrc_v = __builtin_amdgcn_make_buffer_rsrc((void *)prev.v, 0, prev.nrec, RSRC_FLAGS);
         lds_void *dst_k = (lds_void *)(knext + w * Gm::RW * ROWB);
         lds_void *dst_v = (lds_void *)(vcur + w * Gm::RW * ROWB);
+        if constexpr (KV8) fetch_codes(next, prev, j + 1, true, knext, vcur);
         prev = next;
 
         auto operand = [&](auto mc) {
@@ -1208,6 +1366,7 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
             if constexpr (m + PFW == NM) {
                 // every LDS read of this step's tiles has been issued; once they have returned and this
                 // wave's part of the fetched tiles has landed, the waves meet
+                if constexpr (KV8) store_codes(j + 1, true, knext, vcur);
                 __builtin_amdgcn_s_waitcnt(0x0070);           // vmcnt(0) lgkmcnt(0)
                 __syncthreads();
             }
@@ -1232,15 +1391,15 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
                 constexpr int s2 = decltype(sc)::value, m = m0 + s2;
                 fetch(IntC<m>{});
                 f32x2 pv[PPG];
-                if constexpr (s2 == 0) mfma_s_first(Tn[0], op[m % (PFW + 1)], qreg[0][s2], negM[0]);
-                else mfma_s_acc(Tn[0], op[m % (PFW + 1)], qreg[0][s2]);
+                if constexpr (s2 == 0) s_first(Tn[0], op[m % (PFW + 1)], qreg[0][s2], negM[0]);
+                else s_acc(Tn[0], op[m % (PFW + 1)], qreg[0][s2]);
                 __builtin_amdgcn_sched_barrier(0);
                 static_for([&](auto pc) { pv[pc.value] = exp_pair_a(Tc[0], 2 * (PPG * s2 + pc.value)); }, std::make_integer_sequence<int, PPG>{});
                 __builtin_amdgcn_sched_barrier(0);
-                if constexpr (s2 == 0) mfma_s_first(Tn[1], op[m % (PFW + 1)], qreg[1][s2], negM[1]);
-                else mfma_s_acc(Tn[1], op[m % (PFW + 1)], qreg[1][s2]);
+                if constexpr (s2 == 0) s_first(Tn[1], op[m % (PFW + 1)], qreg[1][s2], negM[1]);
+                else s_acc(Tn[1], op[m % (PFW + 1)], qreg[1][s2]);
                 __builtin_amdgcn_sched_barrier(0);
-                if constexpr (i == 0 && s2 < NL) {
+                if constexpr (!KV8 && i == 0 && s2 < NL) {
                     constexpr int li2 = s2 / 2;
                     if constexpr (s2 % 2 == 0) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_k, dst_k, 16, ok.v[li2], 0, li2 * 1024, 0);
                     else __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_v, dst_v, 16, ov.v[li2], 0, li2 * 1024, 0);
@@ -1279,22 +1438,27 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
     // fill: scores of tile 0 for both sub-tiles; K(1), V(0) fetched
     {
         const Src next = tile_src(1);
-        issue_loads(next.k, next.nrec, sK1, offs_k(1));
-        issue_loads(prev.v, prev.nrec, sV0, offs_v(0));
+        if constexpr (KV8) {
+            fetch_codes(next, prev, 1, true, sK1, sV0);
+        } else {
+            issue_loads(next.k, next.nrec, sK1, offs_k(1));
+            issue_loads(prev.v, prev.nrec, sV0, offs_v(0));
+        }
         prev = next;
         pre = tile_src(2);
+        if constexpr (KV8) asm volatile("s_nop 1" : "+v"(negM[0]), "+v"(negM[1]));      // (their zeros are written)
         static_for([&](auto dc) {
             const i32x4 a0 = k_operand(sK0, 0, dc.value), a1 = k_operand(sK0, 1, dc.value);
             if constexpr (dc.value == 0) {
-                mfma_s_first(T0[0], a0, qreg[0][0], negM[0]);
-                mfma_s_first(T0[1], a0, qreg[1][0], negM[1]);
-                mfma_s_first(T1[0], a1, qreg[0][0], negM[0]);
-                mfma_s_first(T1[1], a1, qreg[1][0], negM[1]);
+                s_first(T0[0], a0, qreg[0][0], negM[0]);
+                s_first(T0[1], a0, qreg[1][0], negM[1]);
+                s_first(T1[0], a1, qreg[0][0], negM[0]);
+                s_first(T1[1], a1, qreg[1][0], negM[1]);
             } else {
-                mfma_s_acc(T0[0], a0, qreg[0][dc.value]);
-                mfma_s_acc(T0[1], a0, qreg[1][dc.value]);
-                mfma_s_acc(T1[0], a1, qreg[0][dc.value]);
-                mfma_s_acc(T1[1], a1, qreg[1][dc.value]);
+                s_acc(T0[0], a0, qreg[0][dc.value]);
+                s_acc(T0[1], a0, qreg[1][dc.value]);
+                s_acc(T1[0], a1, qreg[0][dc.value]);
+                s_acc(T1[1], a1, qreg[1][dc.value]);
             }
         }, std::make_integer_sequence<int, Gm::DC>{});
         SETTLE_V2(T0[0], T0[1]);
@@ -1306,6 +1470,7 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
                 if (needs_mask(0, 1, s)) mask_block(T1[s], 0, 1, s);
             }
         }
+        if constexpr (KV8) store_codes(1, true, sK1, sV0);
         __builtin_amdgcn_s_waitcnt(0x0F70);
         __syncthreads();
         static_for([&](auto mc) { op[mc.value] = k_operand(sK1, 0, mc.value); }, std::make_integer_sequence<int, PFW>{});
@@ -1413,37 +1578,40 @@ static hipError_t launch_merge(const AttnParams &p, int G, hipStream_t s) {
     return hipGetLastError();
 }
 
-template <int D, bool NAMED>
+template <int D, bool KV8, bool NAMED>
 static hipError_t launch_w64(const AttnParams &p, int G, hipStream_t s) {
     const unsigned grid = (unsigned)(NAMED ? p.n_units : p.n_tiles * p.splits) * p.Hkv;
-    hipLaunchKernelGGL((attn_bf16_w64_kernel<D, NAMED>), dim3(grid), dim3(256), 0, s, p, G);
+    hipLaunchKernelGGL((attn_bf16_w64_kernel<D, NAMED, KV8>), dim3(grid), dim3(256), 0, s, p, G);
     return hipGetLastError();
 }
 
-template <int D, int NW, int KS, bool PROBE, bool NAMED = false>
+template <int D, bool KV8, int NW, int KS, bool PROBE, bool NAMED = false>
 static hipError_t launch_one(const AttnParams &p, int G, hipStream_t s) {
     const unsigned per_head = PROBE ? p.n_tiles * attn_bf16_units_per_tile(1, G) : NAMED ? p.n_units : p.n_tiles * p.splits;
     const unsigned grid = per_head * p.Hkv;
-    hipLaunchKernelGGL((attn_bf16_kernel<D, NW, KS, PROBE, NAMED>), dim3(grid), dim3(64 * NW * KS), 0, s, p, G);
+    hipLaunchKernelGGL((attn_bf16_kernel<D, NW, KS, PROBE, NAMED, KV8>), dim3(grid), dim3(64 * NW * KS), 0, s, p, G);
     return hipGetLastError();
 }
 
 // a launch of a 32-row form, and the merge of the partial results if its token blocks are cut into ranges
-template <int D, int NW, int KS>
+template <int D, bool KV8, int NW, int KS>
 static hipError_t launch_32(const AttnParams &p, int G, hipStream_t s) {
-    const hipError_t e = p.units != nullptr ? launch_one<D, NW, KS, false, true>(p, G, s) : launch_one<D, NW, KS, false>(p, G, s);
+    const hipError_t e = p.units != nullptr ? launch_one<D, KV8, NW, KS, false, true>(p, G, s) : launch_one<D, KV8, NW, KS, false>(p, G, s);
     return e != hipSuccess || p.n_merges == 0 ? e : launch_merge<D>(p, G, s);
 }
 
-hipError_t launch_attn_bf16(const AttnParams &p0, int head_dim, hipStream_t s) {
-    AttnParams p = p0;
+template <int D, bool KV8>
+static hipError_t launch_attn(const AttnParams &p, int G, hipStream_t s) {
+    if (p.waves == 64) return p.units != nullptr ? launch_w64<D, KV8, true>(p, G, s) : launch_w64<D, KV8, false>(p, G, s);
+    if (p.waves == 8) return launch_32<D, KV8, 8, 1>(p, G, s);
+    return p.key_groups == 2 ? launch_32<D, KV8, 4, 2>(p, G, s) : launch_32<D, KV8, 4, 1>(p, G, s);
+}
+
+hipError_t launch_attn_bf16(const AttnParams &p, int head_dim, hipStream_t s) {
     if (p.n_tiles == 0) return hipSuccess;
     const int G = p.Hq / p.Hkv;
-    if (p.waves == 64 && p.units != nullptr) return head_dim == 128 ? launch_w64<128, true>(p, G, s) : launch_w64<64, true>(p, G, s);
-    if (p.waves == 64) return head_dim == 128 ? launch_w64<128, false>(p, G, s) : launch_w64<64, false>(p, G, s);
-    if (p.waves == 8) return head_dim == 128 ? launch_32<128, 8, 1>(p, G, s) : launch_32<64, 8, 1>(p, G, s);
-    if (p.key_groups == 2) return head_dim == 128 ? launch_32<128, 4, 2>(p, G, s) : launch_32<64, 4, 2>(p, G, s);
-    return head_dim == 128 ? launch_32<128, 4, 1>(p, G, s) : launch_32<64, 4, 1>(p, G, s);
+    if (p.kv8) return head_dim == 128 ? launch_attn<128, true>(p, G, s) : launch_attn<64, true>(p, G, s);
+    return head_dim == 128 ? launch_attn<128, false>(p, G, s) : launch_attn<64, false>(p, G, s);
 }
 
 // Work-groups of a tile per KV head that hold rows of a request of up to `tokens` suffix tokens: group / min(group, 4) of a whole tile.
@@ -1460,9 +1628,9 @@ int attn_bf16_units_per_tile(int num_kv_heads, int group) {
 hipError_t launch_gather_probe(const AttnParams &p, int head_dim, hipStream_t s) {
     if (p.n_tiles == 0) return hipSuccess;
     const int G = p.Hq / p.Hkv;
-    if (p.waves == 4) return head_dim == 128 ? launch_one<128, 4, 1, true>(p, G, s) : launch_one<64, 4, 1, true>(p, G, s);
+    if (p.waves == 4) return head_dim == 128 ? launch_one<128, false, 4, 1, true>(p, G, s) : launch_one<64, false, 4, 1, true>(p, G, s);
     // (the 64-row form cuts the work and stages the tiles as the eight-wave form does: one probe serves both)
-    return head_dim == 128 ? launch_one<128, 8, 1, true>(p, G, s) : launch_one<64, 8, 1, true>(p, G, s);
+    return head_dim == 128 ? launch_one<128, false, 8, 1, true>(p, G, s) : launch_one<64, false, 8, 1, true>(p, G, s);
 }
 
 }  // namespace pbkv

@@ -47,26 +47,33 @@ int fail_hip(hipError_t e, const char *what) {
     return fail(PBKV_ERR_DEVICE, "%s: %s", what, hipGetErrorString(e));
 }
 
-int elt_bytes(int dtype) { return dtype == PBKV_BF16 ? 2 : 4; }
+// of q, k_new, v_new and out
+int elt_bytes(int dtype) { return dtype == PBKV_F32 ? 4 : 2; }
+
+int64_t page_bytes(const pbkv_shape *s) {
+    if (s->dtype == PBKV_BF16_KV8) return pbkv::kv8_page_bytes(s->num_kv_heads, s->head_dim);
+    return (int64_t)2 * s->num_kv_heads * s->page_size * s->head_dim * elt_bytes(s->dtype);
+}
 
 // Shape checks that need no device.  `need_heads` = the call uses the query-head count.
 int check_shape(const pbkv_shape *s, bool need_heads) {
     if (!s) return fail(PBKV_ERR_NULL, "shape is NULL");
-    if (s->dtype != PBKV_BF16 && s->dtype != PBKV_F32) return fail(PBKV_ERR_DTYPE, "unknown dtype %d", s->dtype);
+    if (s->dtype != PBKV_BF16 && s->dtype != PBKV_F32 && s->dtype != PBKV_BF16_KV8) return fail(PBKV_ERR_DTYPE, "unknown dtype %d", s->dtype);
     if (s->page_size != 16) return fail(PBKV_ERR_SHAPE, "page_size %d unsupported (16)", s->page_size);
     if (s->head_dim != 64 && s->head_dim != 128)
         return fail(PBKV_ERR_SHAPE, "head_dim %d unsupported (64, 128)", s->head_dim);
     if (s->num_kv_heads <= 0) return fail(PBKV_ERR_SHAPE, "num_kv_heads %d", s->num_kv_heads);
     if (s->num_pages <= 0) return fail(PBKV_ERR_SHAPE, "num_pages %d", s->num_pages);
-    // the attention kernel addresses pool pages by 32-bit offsets in units of 256 bytes
-    if ((int64_t)s->num_pages * 2 * s->num_kv_heads * s->page_size * s->head_dim * elt_bytes(s->dtype) >= ((int64_t)1 << 40))
-        return fail(PBKV_ERR_LIMIT, "pool of %d pages is 1 TiB or more", s->num_pages);
+    // the attention kernel addresses pool pages by 32-bit offsets in units of 256 bytes, those of an 8-bit pool of 128
+    const int top = s->dtype == PBKV_BF16_KV8 ? 39 : 40;
+    if ((int64_t)s->num_pages * page_bytes(s) >= (int64_t)1 << top)
+        return fail(PBKV_ERR_LIMIT, "pool of %d pages is %s or more", s->num_pages, top == 39 ? "512 GiB" : "1 TiB");
     if (need_heads) {
         if (s->num_q_heads <= 0 || s->num_q_heads % s->num_kv_heads != 0)
             return fail(PBKV_ERR_SHAPE, "num_q_heads %d is not a multiple of num_kv_heads %d",
                         s->num_q_heads, s->num_kv_heads);
         const int G = s->num_q_heads / s->num_kv_heads;
-        if (s->dtype == PBKV_BF16 && !(G == 1 || G == 2 || G == 4 || G == 8 || G == 16))
+        if (s->dtype != PBKV_F32 && !(G == 1 || G == 2 || G == 4 || G == 8 || G == 16))
             return fail(PBKV_ERR_SHAPE, "query/KV head ratio %d unsupported for bf16 (1,2,4,8,16)", G);
     }
     if (s->batch < 0 || s->max_pages_per_req < 0) return fail(PBKV_ERR_SHAPE, "negative batch or table width");
@@ -763,7 +770,7 @@ const char *pbkv_version(void) { return "pbkv 0.2 gfx950"; }
 
 int64_t pbkv_page_bytes(const pbkv_shape *s) {
     if (!s || check_shape(s, false) != PBKV_OK) return 0;
-    return (int64_t)2 * s->num_kv_heads * s->page_size * s->head_dim * elt_bytes(s->dtype);
+    return page_bytes(s);
 }
 
 int pbkv_set_attn_waves(int waves) {
@@ -804,7 +811,8 @@ int pbkv_prefix_prefill(const pbkv_shape *s, const void *q, const void *k_new, c
     p.mirror = nullptr; p.ranges = nullptr; p.mirror_ranges = nullptr; p.key_groups = 1; p.most_parts = 0; p.splits = 1; p.row_groups = 0;
     p.units = nullptr; p.mirror_units = nullptr; p.n_units = 0;
     p.merges = nullptr; p.mirror_merges = nullptr; p.n_merges = 0; p.partial = nullptr;
-    const bool bf16 = s->dtype == PBKV_BF16;
+    p.kv8 = s->dtype == PBKV_BF16_KV8;
+    const bool bf16 = s->dtype != PBKV_F32;
     const int G = s->num_q_heads / s->num_kv_heads;
     const int longest_new = *std::max_element(new_lens, new_lens + s->batch);
     // of the longest request's blocks, with the shape in p.waves
@@ -1010,6 +1018,7 @@ int pbkv_gather_probe(const pbkv_shape *s, const void *k_new, const void *v_new,
     p.mirror = nullptr; p.ranges = nullptr; p.mirror_ranges = nullptr; p.key_groups = 1; p.most_parts = 0; p.splits = 1; p.row_groups = 0;
     p.units = nullptr; p.mirror_units = nullptr; p.n_units = 0;
     p.merges = nullptr; p.mirror_merges = nullptr; p.n_merges = 0; p.partial = nullptr;
+    p.kv8 = 0;
     hipStream_t st = (hipStream_t)stream;
     hipError_t e = pbkv::launch_gather_probe(p, s->head_dim, st);
     int rel = ring_release(lease, st);
@@ -1017,31 +1026,41 @@ int pbkv_gather_probe(const pbkv_shape *s, const void *k_new, const void *v_new,
     return rel;
 }
 
-int pbkv_append_kv(const pbkv_shape *s, const void *k_new, const void *v_new, void *kv_pool,
-                   const int32_t *block_table, const int32_t *prefix_lens, const int32_t *new_lens,
-                   void *stream) {
+}  // extern "C"
+
+namespace {
+
+// Packed K/V rows of the tokens [prefix, prefix + new) of every request to their pool pages (append), or from there (read): the same
+// work list.
+int move_kv(const pbkv_shape *s, void *k_new, void *v_new, void *kv_pool, const int32_t *block_table, const int32_t *prefix_lens,
+            const int32_t *new_lens, void *stream, bool read) {
+    const char *who = read ? "pbkv_read_kv" : "pbkv_append_kv";
     g_err[0] = 0;
     int rc = check_shape(s, false);
     if (rc) return rc;
     if (s->batch == 0) return PBKV_OK;
     if (!k_new || !v_new || !kv_pool || !block_table || !prefix_lens || !new_lens)
-        return fail(PBKV_ERR_NULL, "pbkv_append_kv: NULL argument");
+        return fail(PBKV_ERR_NULL, "%s: NULL argument", who);
     int64_t N = 0;
     if ((rc = check_lens(s, prefix_lens, new_lens, &N))) return rc;
     if (N == 0) return PBKV_OK;
-    if ((rc = check_aligned(k_new, "k_new")) || (rc = check_aligned(v_new, "v_new")) ||
+    if ((rc = check_aligned(k_new, read ? "k" : "k_new")) || (rc = check_aligned(v_new, read ? "v" : "v_new")) ||
         (rc = check_aligned(kv_pool, "kv_pool")))
         return rc;
-    if ((rc = check_device_ptr(k_new, "k_new")) || (rc = check_device_ptr(v_new, "v_new")) ||
+    if ((rc = check_device_ptr(k_new, read ? "k" : "k_new")) || (rc = check_device_ptr(v_new, read ? "v" : "v_new")) ||
         (rc = check_device_ptr(kv_pool, "kv_pool")) || (rc = check_device_ptr(block_table, "block_table")))
         return rc;
 
     hipStream_t st = (hipStream_t)stream;
-    if ((rc = check_not_capturing(st, "pbkv_append_kv"))) return rc;
+    if ((rc = check_not_capturing(st, who))) return rc;
     pbkv::AppendParams p;
     p.k_new = k_new; p.v_new = v_new; p.kv_pool = kv_pool; p.block_table = block_table;
     p.mirror = nullptr;
     p.Hkv = s->num_kv_heads; p.max_pages = s->max_pages_per_req; p.num_pages = s->num_pages;
+    auto launch = [&]() {
+        if (s->dtype == PBKV_BF16_KV8) return read ? pbkv::launch_read_kv8(p, s->head_dim, st) : pbkv::launch_append_kv8(p, s->head_dim, st);
+        return read ? pbkv::launch_read(p, s->head_dim, elt_bytes(s->dtype), st) : pbkv::launch_append(p, s->head_dim, elt_bytes(s->dtype), st);
+    };
 
     DevState *ds = nullptr;
     if ((rc = device_state(&ds))) return rc;
@@ -1052,8 +1071,8 @@ int pbkv_append_kv(const pbkv_shape *s, const void *k_new, const void *v_new, vo
     if (Plan *pl = find_plan(*ds, *sc, PLAN_APPEND, s, 0, prefix_lens, new_lens, &slot)) {
         p.descs = (const pbkv::AppendDesc *)slot;
         p.n_descs = pl->n_a;
-        hipError_t e = pbkv::launch_append(p, s->head_dim, elt_bytes(s->dtype), st);
-        return e == hipSuccess ? PBKV_OK : fail_hip(e, "append launch");
+        hipError_t e = launch();
+        return e == hipSuccess ? PBKV_OK : fail_hip(e, read ? "read launch" : "append launch");
     }
 
     const int P = s->page_size;
@@ -1084,11 +1103,26 @@ int pbkv_append_kv(const pbkv_shape *s, const void *k_new, const void *v_new, vo
         pl->n_a = p.n_descs;
         p.mirror = (pbkv::AppendDesc *)slot;
     }
-    hipError_t e = pbkv::launch_append(p, s->head_dim, elt_bytes(s->dtype), st);
+    hipError_t e = launch();
     int rel = ring_release(lease, st);
-    if (e != hipSuccess) return fail_hip(e, "append launch");
+    if (e != hipSuccess) return fail_hip(e, read ? "read launch" : "append launch");
     if (pl) pl->valid = true;
     return rel;
+}
+
+}  // namespace
+
+extern "C" {
+
+int pbkv_append_kv(const pbkv_shape *s, const void *k_new, const void *v_new, void *kv_pool,
+                   const int32_t *block_table, const int32_t *prefix_lens, const int32_t *new_lens,
+                   void *stream) {
+    return move_kv(s, const_cast<void *>(k_new), const_cast<void *>(v_new), kv_pool, block_table, prefix_lens, new_lens, stream, false);
+}
+
+int pbkv_read_kv(const pbkv_shape *s, const void *kv_pool, const int32_t *block_table, const int32_t *first_tokens,
+                 const int32_t *num_tokens, void *k, void *v, void *stream) {
+    return move_kv(s, k, v, const_cast<void *>(kv_pool), block_table, first_tokens, num_tokens, stream, true);
 }
 
 }  // extern "C"
@@ -1149,7 +1183,7 @@ int pbkv_swap_in_pages(const pbkv_shape *s, const void *host_pages, const int32_
     memcpy(lease.host, page_ids, (size_t)n_pages * sizeof(int32_t));
     hipStream_t st = (hipStream_t)stream;
     hipError_t e = pbkv::launch_swap_in(host_dev, (const int32_t *)lease.dev, n_pages, kv_pool,
-                                        pbkv_page_bytes(s), st);
+                                        page_bytes(s), st);
     int rel = ring_release(lease, st);
     if (e != hipSuccess) return fail_hip(e, "swap-in launch");
     return rel;
@@ -1176,7 +1210,7 @@ int check_decode_args(const pbkv_shape *s, const void *q, const void *kv_pool, c
                       const int32_t *context_lens, void *out, int64_t *total_pages, const char *who) {
     int rc = check_shape(s, true);
     if (rc) return rc;
-    if (s->dtype != PBKV_BF16) return fail(PBKV_ERR_DTYPE, "%s: bf16 only", who);
+    if (s->dtype == PBKV_F32) return fail(PBKV_ERR_DTYPE, "%s: bf16 only", who);
     *total_pages = 0;
     if (s->batch == 0) return PBKV_OK;
     if (!q || !kv_pool || !block_table || !context_lens || !out) return fail(PBKV_ERR_NULL, "%s: NULL argument", who);
@@ -1297,6 +1331,10 @@ int decode_cut(const pbkv_shape *s, const int32_t *context_lens, int64_t total_p
     return PBKV_OK;
 }
 
+hipError_t launch_decode(const pbkv_shape *s, const pbkv::DecodeParams &p, const pbkv::DecodeList &inl, hipStream_t st) {
+    return s->dtype == PBKV_BF16_KV8 ? pbkv::launch_decode_kv8(p, inl, s->head_dim, st) : pbkv::launch_decode_bf16(p, inl, s->head_dim, st);
+}
+
 void fill_decode_reqs(const pbkv_shape *s, const int32_t *context_lens, int32_t slice_pages, pbkv::DecodeReq *reqs) {
     int32_t slice = 0, part = 0;
     for (int r = 0; r < s->batch; r++) {
@@ -1345,7 +1383,7 @@ int pbkv_paged_decode(const pbkv_shape *s, const void *q, const void *kv_pool, c
         p.n_slices = pl->n_a;
         p.slice_pages = pl->n_b;
         if (pl->waves) decode_counters(*sc, &p.counters);
-        hipError_t e = pbkv::launch_decode_bf16(p, inl, s->head_dim, st);
+        hipError_t e = launch_decode(s, p, inl, st);
         return e == hipSuccess ? PBKV_OK : fail_hip(e, "decode launch");
     }
 
@@ -1357,7 +1395,7 @@ int pbkv_paged_decode(const pbkv_shape *s, const void *q, const void *kv_pool, c
     p.slice_pages = cut.slice_pages;
     if (!listed) {
         fill_decode_reqs(s, context_lens, cut.slice_pages, inl.r);
-        hipError_t e = pbkv::launch_decode_bf16(p, inl, s->head_dim, st);
+        hipError_t e = launch_decode(s, p, inl, st);
         return e == hipSuccess ? PBKV_OK : fail_hip(e, "decode launch");
     }
 
@@ -1378,7 +1416,7 @@ int pbkv_paged_decode(const pbkv_shape *s, const void *q, const void *kv_pool, c
         pl->aux = (int64_t)cut.scratch_bytes;
         p.mirror_reqs = (pbkv::DecodeReq *)slot;
     }
-    hipError_t e = pbkv::launch_decode_bf16(p, inl, s->head_dim, st);
+    hipError_t e = launch_decode(s, p, inl, st);
     int rel = ring_release(lease, st);
     if (e != hipSuccess) return fail_hip(e, "decode launch");
     if (pl) pl->valid = true;
@@ -1408,7 +1446,7 @@ int pbkv_swap_out_pages(const pbkv_shape *s, const void *kv_pool, const int32_t 
     memcpy(lease.host, page_ids, (size_t)n_pages * sizeof(int32_t));
     hipStream_t st = (hipStream_t)stream;
     hipError_t e = pbkv::launch_swap_out(kv_pool, (const int32_t *)lease.dev, n_pages, (void *)host_dev,
-                                         pbkv_page_bytes(s), st);
+                                         page_bytes(s), st);
     int rel = ring_release(lease, st);
     if (e != hipSuccess) return fail_hip(e, "swap-out launch");
     return rel;
@@ -1516,7 +1554,7 @@ int pbkv_paged_decode_static(const pbkv_shape *s, const void *q, const void *kv_
         if (e != hipSuccess) return fail_hip(e, "work-list launch");
         p.reqs = (const pbkv::DecodeReq *)(base + STATIC_REQS_OFF);
     }
-    e = pbkv::launch_decode_bf16(p, inl, s->head_dim, st);
+    e = launch_decode(s, p, inl, st);
     return e == hipSuccess ? PBKV_OK : fail_hip(e, "decode launch");
 }
 

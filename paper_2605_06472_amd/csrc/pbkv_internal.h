@@ -9,6 +9,16 @@ namespace pbkv {
 int set_error(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
 void clear_error();
 
+// ---- the 8-bit pool (PBKV_BF16_KV8) ----
+// A page: the e4m3 codes [K, V][KV head][slot][d], then the scale bytes [KV head][slot][K, V], then nothing up to whole 128-byte lines.
+// A scale byte is the biased exponent of a power of two, so a row's values are its codes with another exponent, and bf16 holds
+// them exactly: 3 bits of mantissa, and exponents in [KV8_MIN_EXP, KV8_MAX_EXP] keep every value a normal number.
+constexpr int KV8_MIN_EXP = -111, KV8_MAX_EXP = 119;
+constexpr int64_t kv8_codes_bytes(int num_kv_heads, int head_dim) { return (int64_t)2 * num_kv_heads * 16 * head_dim; }
+constexpr int64_t kv8_page_bytes(int num_kv_heads, int head_dim) {
+    return (kv8_codes_bytes(num_kv_heads, head_dim) + (int64_t)2 * num_kv_heads * 16 + 127) & ~(int64_t)127;
+}
+
 // One unit of attention work: a block of consecutive suffix tokens of one request.
 // Written by the host into pinned memory and read by the kernel through the mapped
 // pointer (32 bytes, two 16-byte loads).
@@ -62,6 +72,7 @@ struct AttnParams {
     const TileDesc *tiles;
     int32_t n_tiles, Hq, Hkv, max_pages, num_pages;
     int32_t waves;   // bf16 kernel: waves per work-group (attn_bf16_waves); the tiles were cut for it
+    int32_t kv8;     // the pool holds 8-bit rows
     int32_t key_groups;   // bf16 kernel, 4 waves: 1, or 2 for work-groups of twice four waves that share a unit's KV tiles out
     TileDesc *mirror;   // device memory that receives a copy of the tiles the launch read, or null
     const RangeDesc *ranges;   // [n_tiles], or null: every unit takes all tiles of its tokens
@@ -102,7 +113,7 @@ struct DecodeParams {
 };
 
 struct AppendParams {
-    const void *k_new, *v_new;
+    void *k_new, *v_new;        // packed rows: read by the append, written by the read
     void *kv_pool;
     const int32_t *block_table;
     const AppendDesc *descs;
@@ -135,8 +146,16 @@ hipError_t launch_append(const AppendParams &p, int head_dim, int elt_bytes, hip
 hipError_t launch_swap_in(const void *host_pages, const int32_t *page_ids_dev, int32_t n_pages,
                           void *kv_pool, int64_t page_bytes, hipStream_t s);
 
-// Paged decode attention (bf16).
+// The way back: pool rows to packed ones.
+hipError_t launch_read(const AppendParams &p, int head_dim, int elt_bytes, hipStream_t s);
+// ... of an 8-bit pool: bf16 rows quantised on their way in, and as bf16 again.
+hipError_t launch_append_kv8(const AppendParams &p, int head_dim, hipStream_t s);
+hipError_t launch_read_kv8(const AppendParams &p, int head_dim, hipStream_t s);
+
+// Paged decode attention (bf16, and over an 8-bit pool).
 hipError_t launch_decode_bf16(const DecodeParams &p, const DecodeList &inl, int head_dim, hipStream_t s);
+hipError_t launch_decode_kv8(const DecodeParams &p, const DecodeList &inl, int head_dim, hipStream_t s);
+hipError_t launch_decode_merge(const DecodeParams &p, const DecodeList &inl, int head_dim, hipStream_t s);
 int64_t decode_partial_floats(int head_dim, int group);   // floats one work-group's partial occupies
 hipError_t launch_clear_words(uint32_t *w, int n, hipStream_t s);
 

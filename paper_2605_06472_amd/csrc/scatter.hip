@@ -72,6 +72,55 @@ hipError_t launch_append(const AppendParams &p, int head_dim, int elt_bytes, hip
     return hipGetLastError();
 }
 
+// Read: the way back, the same runs and parts with source and destination changed over.  The pool row's address needs the page's id
+// before the first load, which the append's stores wait for instead.
+__global__ __launch_bounds__(256) void read_kernel(AppendParams p, int row_shift, int page_size, unsigned parts_per_run, int step_runs, unsigned step_parts) {
+    const int row_chunks = 1 << row_shift;
+    const int per_tok = 2 * p.Hkv * row_chunks;
+    const int64_t page_chunks = (int64_t)per_tok * page_size;
+    u32x4 *kdst = (u32x4 *)p.k_new;
+    u32x4 *vdst = (u32x4 *)p.v_new;
+    int run = (int)(blockIdx.x / parts_per_run);
+    unsigned part_u = blockIdx.x % parts_per_run;
+    for (; run < p.n_descs; run += step_runs, part_u += step_parts, run += part_u >= parts_per_run, part_u -= part_u >= parts_per_run ? parts_per_run : 0) {
+        const int part = (int)part_u;
+        const AppendDesc d = p.descs[run];
+        if (p.mirror != nullptr && part == 0 && threadIdx.x == 0) p.mirror[run] = d;
+        const int total = d.count * per_tok;
+        if (part * APPEND_CHUNKS >= total) continue;
+        const int page_id = p.block_table[(int64_t)d.req * p.max_pages + d.logical_page];
+        const u32x4 *pool = (const u32x4 *)p.kv_pool + (int64_t)clamp_page(page_id, p.num_pages) * page_chunks;
+        u32x4 v[4];
+        u32x4 *dst[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const int idx = part * APPEND_CHUNKS + i * 256 + threadIdx.x;
+            dst[i] = nullptr;
+            if (idx < total) {
+                const int c = idx & (row_chunks - 1);
+                const unsigned row = (unsigned)idx >> row_shift, u = row / (unsigned)p.Hkv;      // (token, K|V, head)
+                const int g = (int)(row - u * p.Hkv), kv = u & 1, t = (int)(u >> 1);
+                v[i] = pool[((int64_t)(kv * p.Hkv + g) * page_size + d.slot0 + t) * row_chunks + c];
+                dst[i] = (kv ? vdst : kdst) + ((d.src_row + t) * p.Hkv + g) * row_chunks + c;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            if (dst[i]) __builtin_nontemporal_store(v[i], dst[i]);
+    }
+}
+
+hipError_t launch_read(const AppendParams &p, int head_dim, int elt_bytes, hipStream_t s) {
+    if (p.n_descs == 0) return hipSuccess;
+    const int row_chunks = head_dim * elt_bytes / 16;
+    const int parts = (16 * 2 * p.Hkv * row_chunks + APPEND_CHUNKS - 1) / APPEND_CHUNKS;
+    const int64_t items = (int64_t)p.n_descs * parts;
+    const int grid = (int)(items < APPEND_MAX_WGS ? items : APPEND_MAX_WGS);
+    hipLaunchKernelGGL(read_kernel, dim3((unsigned)grid), dim3(256), 0, s, p, __builtin_ctz((unsigned)row_chunks), 16, (unsigned)parts,
+                       grid / parts, (unsigned)(grid % parts));
+    return hipGetLastError();
+}
+
 // Swap-in: a work-group moves SWAP_CHUNKS 16-byte chunks of one page at a time from pinned host
 // memory (read over the host link through the mapped pointer) into the page's pool slot.
 // Four independent loads per thread are in flight before the first store.  The grid is small
