@@ -131,7 +131,7 @@ static __device__ __forceinline__ void decode_kv8_slice(const DecodeParams &p, c
     constexpr int E = D / 16;              // d-values of a V row per lane
     constexpr int NB = HB > 0 ? HB : 1;
     constexpr int PR = D + 4;              // floats of a head's row in LDS
-    constexpr int BUFS = D == 64 && HB == 2 ? 2 : 3;   // pages of a wave in registers: one being worked on, the others in flight
+    constexpr int BUFS = 2;                // pages of a wave in registers: one being worked on, the others in flight
     typedef typename CodeRow<D>::type vrow;
 
     const int l = threadIdx.x & 63;
@@ -203,7 +203,7 @@ static __device__ __forceinline__ void decode_kv8_slice(const DecodeParams &p, c
         // codes are read exactly once: streaming loads.  (A line of scales belongs to four KV heads.)
         r.s = *(const u32x2 *)(pool_s + at + 8 * g);
 #pragma unroll
-        for (int j = 0; j < NK; j++) r.k[j] = __builtin_nontemporal_load((const u32x4 *)(kb + koff + 64 * j));
+        for (int j = 0; j < NK; j++) r.k[j] = *(const u32x4 *)(kb + koff + 64 * j);
 #pragma unroll
         for (int i = 0; i < 4; i++) r.v[i] = __builtin_nontemporal_load((const vrow *)(kb + v_in_page + voff + i * D));
     };
@@ -304,24 +304,24 @@ static __device__ __forceinline__ void decode_kv8_slice(const DecodeParams &p, c
             }
     };
 
-    // the next BUFS - 1 pages are in flight while one is being worked on
+    // The next BUFS - 1 pages are in flight while one is being worked on.  Behind the last page it is loaded again (a hit in the caches): where
+    // the load hangs on a condition, the waits for a page's rows have to hold without it too, and wait for the next page's.
     PageRegs rg[BUFS];
+    if (n_mine > 0) {
 #pragma unroll
-    for (int b = 0; b < BUFS - 1; b++)
-        if (b < n_mine) load_page(b, rg[b]);
-    for (int k0 = 0; k0 < n_mine; k0 += BUFS) {
+        for (int b = 0; b < BUFS - 1; b++) load_page(min(b, n_mine - 1), rg[b]);
+        for (int k0 = 0;; k0 += BUFS) {
 #pragma unroll
-        for (int b = 0; b < BUFS; b++) {
-            const int k = k0 + b, next = k + BUFS - 1;
-            if (k < n_mine) {
-                if (next < n_mine) {
-                    if ((next & 63) == 0) ids = load_ids(next >> 6);
-                    load_page(next, rg[(b + BUFS - 1) % BUFS]);
-                }
+            for (int b = 0; b < BUFS; b++) {
+                const int k = k0 + b, next = min(k + BUFS - 1, n_mine - 1);
+                if (k >= n_mine) goto done;
+                if ((next & 63) == 0 && next >= BUFS - 1) ids = load_ids(next >> 6);
+                load_page(next, rg[(b + BUFS - 1) % BUFS]);
                 compute_page(k, rg[b]);
             }
         }
     }
+done:
     leave_wave<D, HB>(acc, M, lsum, G, part[w], part_m[w], part_l[w]);
     finish_slice<D, FUSED>(p, rq, req, kvh, slice, n_slices, G, part, part_m, part_l);
 }
