@@ -205,25 +205,26 @@ struct Codes {
 #pragma unroll
         for (int i = 0; i < NU; i++) s.s[i] = __builtin_amdgcn_raw_buffer_load_b16(rsrc, (slot0 + i * RPU + l / LPR) * 2, 0, 0);
     }
+    // Eight of the lane's codes, number n of CHUNKS, to their place in the tile.
+    static constexpr int CHUNKS = PER_LANE / 8;
     template <bool V>
-    static __device__ __forceinline__ void store(const Rows &r, const Scales &s, char *buf, int w, int l) {
+    static __device__ __forceinline__ void store(const Rows &r, const Scales &s, char *buf, int w, int l, int n) {
+        const int i = n * 8 / CB, h = n % (CB / 8), row = w * Gm::RW + i * RPU + l / LPR;
+        const float scale = __uint_as_float((unsigned)(V ? s.s[i] >> 8 : s.s[i] & 0xff) << 23);
+        bf16x8 x;
 #pragma unroll
-        for (int i = 0; i < NU; i++) {
-            const int row = w * Gm::RW + i * RPU + l / LPR;
-            const float scale = __uint_as_float((unsigned)(V ? s.s[i] >> 8 : s.s[i] & 0xff) << 23);
-#pragma unroll
-            for (int h = 0; h < CB / 8; h++) {
-                bf16x8 x;
-#pragma unroll
-                for (int k = 0; k < 2; k++) {
-                    const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[i][2 * h + k], scale, false);
-                    const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[i][2 * h + k], scale, true);
-                    x[4 * k] = lo[0]; x[4 * k + 1] = lo[1]; x[4 * k + 2] = hi[0]; x[4 * k + 3] = hi[1];
-                }
-                const int chunk = (l % LPR) * (CB / 8) + h;
-                *(bf16x8 *)(buf + row * Gm::ROWB + ((chunk ^ (V ? Gm::swz_v(row) : Gm::swz_k(row))) << 4)) = x;
-            }
+        for (int k = 0; k < 2; k++) {
+            const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[i][2 * h + k], scale, false);
+            const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(r.c[i][2 * h + k], scale, true);
+            x[4 * k] = lo[0]; x[4 * k + 1] = lo[1]; x[4 * k + 2] = hi[0]; x[4 * k + 3] = hi[1];
         }
+        const int chunk = (l % LPR) * (CB / 8) + h;
+        *(bf16x8 *)(buf + row * Gm::ROWB + ((chunk ^ (V ? Gm::swz_v(row) : Gm::swz_k(row))) << 4)) = x;
+    }
+    template <bool V>
+    static __device__ __forceinline__ void store_all(const Rows &r, const Scales &s, char *buf, int w, int l) {
+#pragma unroll
+        for (int n = 0; n < CHUNKS; n++) store<V>(r, s, buf, w, l, n);
     }
 };
 #endif
@@ -381,33 +382,39 @@ void attn_bf16_kernel(AttnParams p, int G) {
     };
     auto offs_k = [&](int t) { Offs o;
 #pragma unroll
-        for (int i = 0; i < Gm::NI; i++) o.v[i] = t < TP ? vk_p[i] : vk_s[i];
+        for (int i = 0; i < Gm::NI; i++) o.v[i] = !KV8 && t < TP ? vk_p[i] : vk_s[i];
         return o; };
     auto offs_v = [&](int t) { Offs o;
 #pragma unroll
-        for (int i = 0; i < Gm::NI; i++) o.v[i] = t < TP ? vv_p[i] : vv_s[i];
+        for (int i = 0; i < Gm::NI; i++) o.v[i] = !KV8 && t < TP ? vv_p[i] : vv_s[i];
         return o; };
 
-    // An 8-bit pool: the rows of K tile t and of V tile t - 1, and the scales of tile t, whose V rows are the next tile's turn; prefix rows into
-    // registers, and from there to LDS when the step's arithmetic has been issued, suffix rows straight to LDS.
+    // An 8-bit pool.  Between two steps the codes of what the next one writes to LDS -- K tile j + 1, V tile j -- are on their way into
+    // registers, asked for a step ahead; suffix rows go straight to LDS as ever.  A step of prefix tiles alone
+    // converts and stores them between its MFMAs, the others in one go behind them.
     using Cd = Codes<D, NW>;
     [[maybe_unused]] typename Cd::Rows codes_k, codes_v;
     [[maybe_unused]] typename Cd::Scales scales_k, scales_v;
-    auto fetch_codes = [&](const auto &k, const auto &v, int t, bool with_v, char *kbuf, char *vbuf) __attribute__((always_inline)) {
-        if (t < TP) {
-            Cd::load(codes_k, k.k, k.nrec, slot0, l);
-            Cd::load_scales(scales_k, k.scales, k.nrec, slot0, l);
-        } else {
-            issue_loads(k.k, k.nrec, kbuf, offs_k(t));
-        }
-        if (!with_v) return;
-        if (t - 1 < TP) Cd::load(codes_v, v.v, v.nrec, slot0, l);
-        else issue_loads(v.v, v.nrec, vbuf, offs_v(t - 1));
-    };
-    auto store_codes = [&](int t, bool with_v, char *kbuf, char *vbuf) __attribute__((always_inline)) {
-        if (t < TP) Cd::template store<false>(codes_k, scales_k, kbuf, w, l);
-        if (with_v && t - 1 < TP) Cd::template store<true>(codes_v, scales_v, vbuf, w, l);
+    auto request_k = [&](const auto &src, int t) __attribute__((always_inline)) {      // (past the last tile: no bytes)
         scales_v = scales_k;
+        const int bytes = t < kt1 ? src.nrec : 0;
+        Cd::load(codes_k, src.k, bytes, slot0, l);
+        if constexpr (KV8) Cd::load_scales(scales_k, src.scales, bytes, slot0, l);
+    };
+    auto request_v = [&](const auto &src, int t) __attribute__((always_inline)) { Cd::load(codes_v, src.v, t < kt1 ? src.nrec : 0, slot0, l); };
+    // K tile t and V tile t - 1: asked for, brought to LDS
+    auto request = [&](const auto &k, const auto &v, int t) __attribute__((always_inline)) {
+        if (t < TP) request_k(k, t);
+        else scales_v = scales_k;
+        if (t - 1 < TP) request_v(v, t - 1);
+    };
+    auto direct = [&](const auto &k, const auto &v, int t, char *kbuf, char *vbuf) __attribute__((always_inline)) {
+        if (t >= TP) issue_loads(k.k, k.nrec, kbuf, offs_k(t));
+        if (t - 1 >= TP) issue_loads(v.v, v.nrec, vbuf, offs_v(t - 1));
+    };
+    auto store_codes = [&](int t, char *kbuf, char *vbuf) __attribute__((always_inline)) {
+        if (t < TP) Cd::template store_all<false>(codes_k, scales_k, kbuf, w, l);
+        if (t - 1 < TP) Cd::template store_all<true>(codes_v, scales_v, vbuf, w, l);
     };
 
     // ---- running state --------------------------------------------------------------------
@@ -425,6 +432,8 @@ void attn_bf16_kernel(AttnParams p, int G) {
     f32x16 negM;
 #pragma unroll
     for (int r = 0; r < 16; r++) negM[r] = 0.f;
+    // An 8-bit pool: scores come from exact Q and 0, and scale and reference are one FMA in front of the exponential.
+    [[maybe_unused]] float ref = 0.f;
 
     // ---- per-lane LDS operand offsets (the swizzle makes them lane- and chunk-specific) ---
     // K operand (kb, dc): row 32*kb + li, chunk 2*dc + lh
@@ -471,8 +480,12 @@ void attn_bf16_kernel(AttnParams p, int G) {
     Src prev{};
     if (KS == 1 || kt0 < kt1) {
         prev = tile_src(kt0);
-        if constexpr (KV8) fetch_codes(prev, prev, kt0, false, sK0, nullptr);
-        else issue_loads(prev.k, prev.nrec, sK0, offs_k(kt0));
+        if constexpr (KV8) {
+            if (kt0 < TP) request_k(prev, kt0);
+            else issue_loads(prev.k, prev.nrec, sK0, offs_k(kt0));
+        } else {
+            issue_loads(prev.k, prev.nrec, sK0, offs_k(kt0));
+        }
     }
     __builtin_amdgcn_sched_barrier(0);
     // ---- Q^T operands, pre-scaled: lane (li, lh) holds c * Q[row li][16*dc + 8*lh .. +7] ----
@@ -514,7 +527,8 @@ void attn_bf16_kernel(AttnParams p, int G) {
 #pragma unroll
         for (int dc = 0; dc < Gm::DC; dc++)
 #pragma unroll
-            for (int e = 0; e < 8; e++) qreg[dc][e] = (__bf16)((float)qreg[dc][e] * c);
+            for (int e = 0; e < 8; e++)
+                if constexpr (!KV8) qreg[dc][e] = (__bf16)((float)qreg[dc][e] * c);
     }
     // zero the rows of the V buffers that this wave will load, once: rows past the last key are never loaded, and 0 *
     // stale bits must not be able to produce a NaN in the PV product
@@ -524,7 +538,7 @@ void attn_bf16_kernel(AttnParams p, int G) {
         *(uint4 *)(sV1 + (w * Gm::NI + i) * 1024 + l * 16) = make_uint4(0, 0, 0, 0);
     }
     if constexpr (KV8) {
-        if (KS == 1 || kt0 < kt1) store_codes(kt0, false, sK0, nullptr);
+        if ((KS == 1 || kt0 < kt1) && kt0 < TP) Cd::template store_all<false>(codes_k, scales_k, sK0, w, l);
     }
     __syncthreads();
 
@@ -591,11 +605,17 @@ void attn_bf16_kernel(AttnParams p, int G) {
     // rescaled, and its probabilities are formed again.  The first block is always redone, which sets
     // M to its row maximum whatever the magnitude of the scores, and so is every block up to the first in which
     // a row has a score above -inf (a range may begin with keys that count nothing).
+    auto start = [&]() __attribute__((always_inline)) { return KV8 ? f32x16{} : negM; };      // what a chain of score products adds to
+    auto prob = [&](float x) __attribute__((always_inline)) {
+        if constexpr (KV8) return __builtin_amdgcn_exp2f(fmaf(x, c, -ref));
+        else return __builtin_amdgcn_exp2f(x);
+    };
     auto redo_block = [&](f32x16 &Tc, f32x16 &Tn, bf16x8 (&Pp)[2]) __attribute__((always_inline)) {
         float mxp = Tn[0];
 #pragma unroll
         for (int r = 1; r < 16; r++) mxp = fmaxf(mxp, Tn[r]);
         mxp = xmax32(mxp);
+        if constexpr (KV8) mxp = fmaf(mxp, c, -ref);
         const bool first = xsum32(l_part) == 0.f;                 // nothing of this row has counted so far
         const bool none = first && mxp == -INFINITY;
         const float d = none ? 0.f : (first ? mxp : fmaxf(mxp, 0.f));      // later moves never lower the reference
@@ -605,15 +625,19 @@ void attn_bf16_kernel(AttnParams p, int G) {
         // whole-vector updates: the 16-register accumulator tuples stay where they are
 #pragma unroll
         for (int db = 0; db < Gm::DB; db++) O[db] *= alpha;
-        Tn -= d;
-        Tc -= d;
-        negM -= d;
+        if constexpr (KV8) {
+            ref += d;
+        } else {
+            Tn -= d;
+            Tc -= d;
+            negM -= d;
+        }
         lb = 0.f;
 #pragma unroll
         for (int r = 0; r < 16; r += 2) {
             f32x2 pv;
-            pv[0] = __builtin_amdgcn_exp2f(Tn[r]);
-            pv[1] = __builtin_amdgcn_exp2f(Tn[r + 1]);
+            pv[0] = prob(Tn[r]);
+            pv[1] = prob(Tn[r + 1]);
             const bf16x2 pk = __builtin_convertvector(pv, bf16x2);
             Pp[r / 8][r % 8] = pk[0];
             Pp[r / 8][r % 8 + 1] = pk[1];
@@ -632,19 +656,29 @@ void attn_bf16_kernel(AttnParams p, int G) {
     // for the product halves) from ONE stream that runs PF MFMAs ahead, across the half and
     // iteration boundaries, so only the start of a step exposes LDS latency.
     //
-    auto step = [&](int j, char *kcur, char *knext, char *vprev, char *vcur) __attribute__((always_inline)) {
+    [[maybe_unused]] Src ahead{};                          // 8-bit pool: source of tile j + 1, prev being that of tile j
+    auto src_of_next = [&](auto kv8, int j) __attribute__((always_inline)) {
+        if constexpr (kv8.value) return ahead;
+        else return tile_src(j + 1);
+    };
+    // kind, 8-bit pools: 1 a step between prefix tiles alone (K tile j + 1 is one), 2 one behind the prefix (V tile j is suffix rows), 0 any
+    auto step = [&](auto kind, int j, char *kcur, char *knext, char *vprev, char *vcur) __attribute__((always_inline)) {
+        constexpr bool CODES = KV8 && decltype(kind)::value == 1, DIRECT = !KV8 || decltype(kind)::value == 2;
         constexpr int NM = 4 * H;                          // MFMAs per step
         constexpr int LD_SP = H / (2 * Gm::NI);            // MFMAs between two tile loads
         static_assert(LD_SP >= 1, "the tile loads of a step fit its first half iteration");
         // sources: K(j+1) now, V(j) from what the previous step found for tile j
-        const Src next = tile_src(j + 1);
+        const Src next = src_of_next(IntC<KV8>{}, j);
         const Offs ok = offs_k(j + 1), ov = offs_v(j);
-        const bool masked = j >= TPF;                      // tile j is not a full prefix tile
+        const bool masked = !CODES && j >= TPF;            // tile j is not a full prefix tile
         const auto rsrc_k = __builtin_amdgcn_make_buffer_rsrc((void *)next.k, 0, next.nrec, RSRC_FLAGS);
         const auto rsrc_v = __builtin_amdgcn_make_buffer_rsrc((void *)prev.v, 0, prev.nrec, RSRC_FLAGS);
         lds_void *dst_k = (lds_void *)(knext + w * Gm::RW * ROWB);
         lds_void *dst_v = (lds_void *)(vcur + w * Gm::RW * ROWB);
-        if constexpr (KV8) fetch_codes(next, prev, j + 1, true, knext, vcur);
+        if constexpr (KV8) {
+            if constexpr (!CODES && !DIRECT) direct(next, prev, j + 1, knext, vcur);
+            ahead = tile_src(j + 2);
+        }
         prev = next;
 
         // operand stream: entry m feeds MFMA m of the step
@@ -665,8 +699,8 @@ void attn_bf16_kernel(AttnParams p, int G) {
             lb = 0.f;
             auto exp_pair = [&](int r) {                  // scores r, r+1 of the pending block
                 f32x2 pv;
-                pv[0] = __builtin_amdgcn_exp2f(Tc[r]);
-                pv[1] = __builtin_amdgcn_exp2f(Tc[r + 1]);
+                pv[0] = prob(Tc[r]);
+                pv[1] = prob(Tc[r + 1]);
                 const bf16x2 pk = __builtin_convertvector(pv, bf16x2);
                 Pc[r / 8][r % 8] = pk[0];
                 Pc[r / 8][r % 8 + 1] = pk[1];
@@ -679,15 +713,17 @@ void attn_bf16_kernel(AttnParams p, int G) {
                 constexpr int s2 = decltype(sc)::value, m = m0 + s2;
                 if constexpr (m + PF < NM) op[(m + PF) % (PF + 1)] = operand(IntC<m + PF>{});
                 MFMA_PRIO(1);
-                Tn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[m % (PF + 1)], qreg[s2], s2 == 0 ? negM : Tn, 0, 0, 0);
+                Tn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[m % (PF + 1)], qreg[s2], s2 == 0 ? start() : Tn, 0, 0, 0);
                 MFMA_PRIO(0);
                 // all tile loads of the step go out in its first half iteration, K and V rows
                 // alternating, one every LD_SP MFMAs: they have the rest of the step to land
-                if constexpr (!KV8 && i == 0 && s2 % LD_SP == 0) {
+                if constexpr (DIRECT && i == 0 && s2 % LD_SP == 0) {
                     constexpr int q = s2 / LD_SP, li2 = q / 2;
                     if constexpr (q % 2 == 0) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_k, dst_k, 16, ok.v[li2], 0, li2 * 1024, 0);
                     else __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_v, dst_v, 16, ov.v[li2], 0, li2 * 1024, 0);
                 }
+                if constexpr (CODES && i == 1 && s2 % (H / Cd::CHUNKS) == 0)
+                    Cd::template store<false>(codes_k, scales_k, knext, w, l, s2 / (H / Cd::CHUNKS));
                 // four score pairs over H steps
                 if constexpr (H == 8) { if constexpr (s2 % 2 == 0) exp_pair(s2); }
                 else exp_pair(2 * s2);
@@ -696,8 +732,8 @@ void attn_bf16_kernel(AttnParams p, int G) {
                 constexpr int s2 = decltype(sc)::value, m = m0 + s2;
                 if constexpr (m == 0) __builtin_amdgcn_sched_group_barrier(SG_DSRD, PF, 0);
                 __builtin_amdgcn_sched_group_barrier(SG_MFMA, 1, 0);
-                if constexpr (!KV8 && i == 0 && s2 % LD_SP == 0) __builtin_amdgcn_sched_group_barrier(SG_VMRD, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(SG_VALU, 16 / H, 0);
+                if constexpr (DIRECT && i == 0 && s2 % LD_SP == 0) __builtin_amdgcn_sched_group_barrier(SG_VMRD, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(SG_VALU, KV8 ? 24 / H + (CODES && i == 1 ? 4 * Cd::CHUNKS / H + 1 : 0) : 16 / H, 0);
                 if constexpr (m + PF < NM) __builtin_amdgcn_sched_group_barrier(SG_DSRD, ((m + PF) / H) & 1 ? 2 : 1, 0);
             }, std::make_integer_sequence<int, H>{});
             // the probabilities are only consumed an iteration later; keep their computation here,
@@ -714,6 +750,8 @@ void attn_bf16_kernel(AttnParams p, int G) {
             static_for([&](auto sc) {
                 constexpr int s2 = decltype(sc)::value, m = m0 + H + s2;
                 if constexpr (m + PF < NM) op[(m + PF) % (PF + 1)] = operand(IntC<m + PF>{});
+                if constexpr (CODES && i == 1 && s2 % (H / Cd::CHUNKS) == 0)
+                    Cd::template store<true>(codes_v, scales_v, vcur, w, l, s2 / (H / Cd::CHUNKS));
                 MFMA_PRIO(1);
                 O[s2 % Gm::DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[m % (PF + 1)], Pp[s2 / Gm::DB], O[s2 % Gm::DB], 0, 0, 0);
                 MFMA_PRIO(0);
@@ -736,7 +774,7 @@ void attn_bf16_kernel(AttnParams p, int G) {
             static_for([&](auto sc) {
                 constexpr int s2 = decltype(sc)::value, m = m0 + H + s2;
                 __builtin_amdgcn_sched_group_barrier(SG_MFMA, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(SG_VALU, s2 == H - 1 ? 12 : 16 / H, 1);
+                __builtin_amdgcn_sched_group_barrier(SG_VALU, s2 == H - 1 ? 12 : KV8 ? 24 / H + (CODES && i == 1 ? 4 * Cd::CHUNKS / H + 1 : 0) : 16 / H, 1);
                 if constexpr (m + PF < NM) __builtin_amdgcn_sched_group_barrier(SG_DSRD, ((m + PF) / H) & 1 ? 2 : 1, 1);
             }, std::make_integer_sequence<int, H>{});
             PIN_V(Pc[1]);
@@ -745,8 +783,16 @@ void attn_bf16_kernel(AttnParams p, int G) {
         };
         iteration(IntC<0>{}, T1, T0, P1, P0);             // block 0 is redone before its PV product
         iteration(IntC<1>{}, T0, T1, P0, P1);
-        if constexpr (KV8) store_codes(j + 1, true, knext, vcur);
-        __builtin_amdgcn_s_waitcnt(0x0F70);               // vmcnt(0): K(j+1), V(j) are in LDS
+        if constexpr (!CODES) {
+            if constexpr (!DIRECT) store_codes(j + 1, knext, vcur);
+            __builtin_amdgcn_s_waitcnt(0x0F70);           // vmcnt(0): K(j+1), V(j) are in LDS
+        }
+        if constexpr (CODES) {
+            request_k(ahead, j + 2);
+            request_v(prev, j + 1);
+        } else if constexpr (!DIRECT) {
+            request(ahead, prev, j + 2);
+        }
         __syncthreads();                                  // ... and every wave is done with K(j), V(j-1)
     };
     // fill: scores of the two blocks of tile 0 (from the reference 0; the first full or drain step
@@ -754,7 +800,9 @@ void attn_bf16_kernel(AttnParams p, int G) {
     if (KS == 1 || kt0 < kt1) {
         const Src next = tile_src(kt0 + 1);
         if constexpr (KV8) {
-            fetch_codes(next, prev, kt0 + 1, true, sK1, sV0);
+            request(next, prev, kt0 + 1);
+            direct(next, prev, kt0 + 1, sK1, sV0);
+            ahead = tile_src(kt0 + 2);
         } else {
             issue_loads(next.k, next.nrec, sK1, offs_k(kt0 + 1));
             issue_loads(prev.v, prev.nrec, sV0, offs_v(kt0));
@@ -763,39 +811,63 @@ void attn_bf16_kernel(AttnParams p, int G) {
     }
     if (active && (KS == 1 || kt0 < kt1)) {
         static_for([&](auto dc) {
-            T0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(sK0, 0, dc.value), qreg[dc.value], dc.value == 0 ? negM : T0, 0, 0, 0);
-            T1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(sK0, 1, dc.value), qreg[dc.value], dc.value == 0 ? negM : T1, 0, 0, 0);
+            T0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(sK0, 0, dc.value), qreg[dc.value], dc.value == 0 ? start() : T0, 0, 0, 0);
+            T1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_operand(sK0, 1, dc.value), qreg[dc.value], dc.value == 0 ? start() : T1, 0, 0, 0);
         }, std::make_integer_sequence<int, Gm::DC>{});
         if (kt0 >= TPF) {
             if (needs_mask(kt0, 0)) mask_block(T0, kt0, 0);
             if (needs_mask(kt0, 1)) mask_block(T1, kt0, 1);
         }
-        if constexpr (KV8) store_codes(kt0 + 1, true, sK1, sV0);
+        if constexpr (KV8) store_codes(kt0 + 1, sK1, sV0);
         __builtin_amdgcn_s_waitcnt(0x0F70);
+        if constexpr (KV8) request(ahead, prev, kt0 + 2);
         __syncthreads();
         // full steps kt0 + 1 .. kt1 - 1, in pairs so that the LDS buffers are compile-time constants
-        for (int j = kt0 + 1; j < kt1; j += 2) {
-            step(j, sK1, sK0, sV0, sV1);
-            if (j + 1 < kt1) step(j + 1, sK0, sK1, sV1, sV0);
+        if constexpr (KV8) {
+            int j = kt0 + 1;
+            for (; j + 1 < kt1 && j + 3 < TP; j += 2) {    // (what both steps ask for lies in the prefix, too)
+                step(IntC<1>{}, j, sK1, sK0, sV0, sV1);
+                step(IntC<1>{}, j + 1, sK0, sK1, sV1, sV0);
+            }
+            for (; j < kt1 && j < TP; j += 2) {
+                step(IntC<0>{}, j, sK1, sK0, sV0, sV1);
+                if (j + 1 < kt1) step(IntC<0>{}, j + 1, sK0, sK1, sV1, sV0);
+            }
+            for (; j < kt1; j += 2) {
+                step(IntC<2>{}, j, sK1, sK0, sV0, sV1);
+                if (j + 1 < kt1) step(IntC<2>{}, j + 1, sK0, sK1, sV1, sV0);
+            }
+        } else {
+            for (int j = kt0 + 1; j < kt1; j += 2) {
+                step(IntC<0>{}, j, sK1, sK0, sV0, sV1);
+                if (j + 1 < kt1) step(IntC<0>{}, j + 1, sK0, sK1, sV1, sV0);
+            }
         }
     } else {
         // a wave without rows fetches its part of the tiles for the others
         if constexpr (KV8) {
-            if (KS == 1 || kt0 < kt1) store_codes(kt0 + 1, true, sK1, sV0);
+            if (KS == 1 || kt0 < kt1) store_codes(kt0 + 1, sK1, sV0);
         }
         __builtin_amdgcn_s_waitcnt(0x0F70);
+        if constexpr (KV8) {
+            if (KS == 1 || kt0 < kt1) request(ahead, prev, kt0 + 2);
+        }
         __syncthreads();
         for (int j = kt0 + 1; j < kt1; j++) {
-            const Src next = tile_src(j + 1);
-            const bool odd = (j - kt0) & 1;
             if constexpr (KV8) {
-                fetch_codes(next, prev, j + 1, true, odd ? sK0 : sK1, odd ? sV1 : sV0);
-                store_codes(j + 1, true, odd ? sK0 : sK1, odd ? sV1 : sV0);
+                const bool odd = (j - kt0) & 1;
+                direct(ahead, prev, j + 1, odd ? sK0 : sK1, odd ? sV1 : sV0);
+                store_codes(j + 1, odd ? sK0 : sK1, odd ? sV1 : sV0);
+                prev = ahead;
+                ahead = tile_src(j + 2);
+                request(ahead, prev, j + 2);
             } else {
+                const Src next = tile_src(j + 1);
+                const bool odd = (j - kt0) & 1;
                 issue_loads(next.k, next.nrec, odd ? sK0 : sK1, offs_k(j + 1));
                 issue_loads(prev.v, prev.nrec, odd ? sV1 : sV0, offs_v(j));
+                prev = next;
             }
-            prev = next;
             __builtin_amdgcn_s_waitcnt(0x0F70);
             __syncthreads();
         }
@@ -811,8 +883,8 @@ void attn_bf16_kernel(AttnParams p, int G) {
 #pragma unroll
             for (int r = 0; r < 16; r += 2) {
                 f32x2 pv;
-                pv[0] = __builtin_amdgcn_exp2f(Tc[r]);
-                pv[1] = __builtin_amdgcn_exp2f(Tc[r + 1]);
+                pv[0] = prob(Tc[r]);
+                pv[1] = prob(Tc[r + 1]);
                 const bf16x2 pk = __builtin_convertvector(pv, bf16x2);
                 Pc[r / 8][r % 8] = pk[0];
                 Pc[r / 8][r % 8 + 1] = pk[1];
@@ -841,7 +913,7 @@ void attn_bf16_kernel(AttnParams p, int G) {
     // rows 16-31 are d = D/2 + 16*db + (row - 16)
     float lsum = xsum32(l_part);
     // (a row that no key of the range counts for has no reference: any other range's must win the maximum)
-    float M = lsum == 0.f ? -__FLT_MAX__ : -negM[0];
+    float M = lsum == 0.f ? -__FLT_MAX__ : KV8 ? ref : -negM[0];
     // what the wave leaves of O blocks [DB0, DB1): of a range of the keys the unnormalised output, to the partial-result
     // buffer in register order (whole 1 KiB runs per wave; attn_merge_kernel reads them in the same order), with
     // reference and row sum; of all keys the result
@@ -974,9 +1046,9 @@ static __device__ __forceinline__ void mfma_s_first(f32x16 &d, const i32x4 &a, c
 static __device__ __forceinline__ void mfma_s_acc(f32x16 &d, const i32x4 &a, const i32x4 &b) {
     asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "v"(b));
 }
-// the same with b in accumulation registers
-static __device__ __forceinline__ void mfma_s_first_q(f32x16 &d, const i32x4 &a, const i32x4 &b, const f32x16 &c) {
-    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %3" : "=&v"(d) : "v"(a), "a"(b), "v"(c));
+// the same with b in accumulation registers, and a first one that adds to nothing
+static __device__ __forceinline__ void mfma_s_first_q(f32x16 &d, const i32x4 &a, const i32x4 &b) {
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(d) : "v"(a), "a"(b));
 }
 static __device__ __forceinline__ void mfma_s_acc_q(f32x16 &d, const i32x4 &a, const i32x4 &b) {
     asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "a"(b));
@@ -984,6 +1056,39 @@ static __device__ __forceinline__ void mfma_s_acc_q(f32x16 &d, const i32x4 &a, c
 // d += a b, outputs: accumulator in accumulation registers, operands in vector registers
 static __device__ __forceinline__ void mfma_o_acc(f32x16 &d, const i32x4 &a, const i32x4 &b) {
     asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(d) : "v"(a), "v"(b));
+}
+// A group of an 8-bit pool's step in one statement, so that the compiler puts no waits of its own between its parts (a statement reads what one before it
+// wrote): the MFMAs of both sub-tiles, between them N score pairs' exponentials exp2(c x - m), each one FMA first, behind them
+// the packs, an instruction after the exponentials as those have to be.
+#define KV8_PAIR(x, y, s, t) "v_fma_f32 " x ", " s ", %[c], -%[m]\n\tv_fma_f32 " y ", " t ", %[c], -%[m]\n\tv_exp_f32 " x ", " x "\n\tv_exp_f32 " y ", " y "\n\t"
+#define KV8_GROUP1(D0, D1, C0, C1, CLASS, B) \
+    asm volatile("v_mfma_f32_32x32x16_bf16 %[d0], %[a], %[b0], " C0 "\n\t" KV8_PAIR("%[x]", "%[y]", "%[s]", "%[t]") \
+                 "v_mfma_f32_32x32x16_bf16 %[d1], %[a], %[b1], " C1 "\n\tv_cvt_pk_bf16_f32 %[p], %[x], %[y]" \
+                 : [d0] CLASS(D0), [d1] CLASS(D1), [x] "=&v"(x0), [y] "=&v"(y0), [p] "=&v"(bits[0]) \
+                 : [a] "v"(a), [b0] B(b0), [b1] B(b1), [s] "v"(Tc[r]), [t] "v"(Tc[r + 1]), [c] "s"(c), [m] "v"(m))
+#define KV8_GROUP2(D0, D1, C0, C1, CLASS, B) \
+    asm volatile("v_mfma_f32_32x32x16_bf16 %[d0], %[a], %[b0], " C0 "\n\t" KV8_PAIR("%[x]", "%[y]", "%[s]", "%[t]") KV8_PAIR("%[x1]", "%[y1]", "%[s1]", "%[t1]") \
+                 "v_mfma_f32_32x32x16_bf16 %[d1], %[a], %[b1], " C1 "\n\tv_cvt_pk_bf16_f32 %[p], %[x], %[y]\n\tv_cvt_pk_bf16_f32 %[p1], %[x1], %[y1]" \
+                 : [d0] CLASS(D0), [d1] CLASS(D1), [x] "=&v"(x0), [y] "=&v"(y0), [x1] "=&v"(x1), [y1] "=&v"(y1), [p] "=&v"(bits[0]), [p1] "=&v"(bits[1]) \
+                 : [a] "v"(a), [b0] B(b0), [b1] B(b1), [s] "v"(Tc[r]), [t] "v"(Tc[r + 1]), [s1] "v"(Tc[r + 2]), [t1] "v"(Tc[r + 3]), [c] "s"(c), [m] "v"(m))
+template <int N>
+static __device__ __forceinline__ void kv8_group_s(bool first, f32x16 (&d)[2], const i32x4 &a, const i32x4 &b0, const i32x4 &b1, const f32x16 &Tc, int r, float c, float m, int (&bits)[2]) {
+    float x0, y0, x1, y1;
+    (void)x1, (void)y1;
+    if constexpr (N == 1) {
+        if (first) KV8_GROUP1(d[0], d[1], "0", "0", "=&v", "a");
+        else KV8_GROUP1(d[0], d[1], "%[d0]", "%[d1]", "+v", "a");
+    } else {
+        if (first) KV8_GROUP2(d[0], d[1], "0", "0", "=&v", "a");
+        else KV8_GROUP2(d[0], d[1], "%[d0]", "%[d1]", "+v", "a");
+    }
+}
+template <int N>
+static __device__ __forceinline__ void kv8_group_o(f32x16 &d0, f32x16 &d1, const i32x4 &a, const i32x4 &b0, const i32x4 &b1, const f32x16 &Tc, int r, float c, float m, int (&bits)[2]) {
+    float x0, y0, x1, y1;
+    (void)x1, (void)y1;
+    if constexpr (N == 1) KV8_GROUP1(d0, d1, "%[d0]", "%[d1]", "+a", "v");
+    else KV8_GROUP2(d0, d1, "%[d0]", "%[d1]", "+a", "v");
 }
 // "whatever wrote these registers has finished": 36 idle cycles tied to the values by operands
 #define SETTLE_V2(x, y) asm volatile("s_nop 15\n\ts_nop 15\n\ts_nop 3" : "+v"(x), "+v"(y))
@@ -1047,7 +1152,7 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
             const bf16x8 raw = *(const bf16x8 *)(qp + dc * 16);
             bf16x8 sc;
 #pragma unroll
-            for (int e = 0; e < 8; e++) sc[e] = (__bf16)((float)raw[e] * c);
+            for (int e = 0; e < 8; e++) sc[e] = KV8 ? raw[e] : (__bf16)((float)raw[e] * c);
             qreg[s][dc] = as_i(sc);
         }
     }
@@ -1062,7 +1167,7 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
             for (int dc = 0; dc < Gm::DC; dc++) asm volatile("" : "+a"(qreg[s][dc]));
     }
     auto s_first = [](f32x16 &d, const i32x4 &a, const i32x4 &b, const f32x16 &c) __attribute__((always_inline)) {
-        if constexpr (KV8) mfma_s_first_q(d, a, b, c);
+        if constexpr (KV8) mfma_s_first_q(d, a, b);
         else mfma_s_first(d, a, b, c);
     };
     auto s_acc = [](f32x16 &d, const i32x4 &a, const i32x4 &b) __attribute__((always_inline)) {
@@ -1145,32 +1250,37 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
     };
     auto offs_k = [&](int t) { Offs o;
 #pragma unroll
-        for (int i = 0; i < Gm::NI; i++) o.v[i] = t < TP ? vk_p[i] : vk_s[i];
+        for (int i = 0; i < Gm::NI; i++) o.v[i] = !KV8 && t < TP ? vk_p[i] : vk_s[i];
         return o; };
     auto offs_v = [&](int t) { Offs o;
 #pragma unroll
-        for (int i = 0; i < Gm::NI; i++) o.v[i] = t < TP ? vv_p[i] : vv_s[i];
+        for (int i = 0; i < Gm::NI; i++) o.v[i] = !KV8 && t < TP ? vv_p[i] : vv_s[i];
         return o; };
 
-    // (as in the kernel above)
+    // an 8-bit pool's codes (as in the kernel above)
     using Cd = Codes<D, NW>;
     [[maybe_unused]] typename Cd::Rows codes_k, codes_v;
     [[maybe_unused]] typename Cd::Scales scales_k, scales_v;
-    auto fetch_codes = [&](const auto &k, const auto &v, int t, bool with_v, char *kbuf, char *vbuf) __attribute__((always_inline)) {
-        if (t < TP) {
-            Cd::load(codes_k, k.k, k.nrec, slot0, l);
-            Cd::load_scales(scales_k, k.scales, k.nrec, slot0, l);
-        } else {
-            issue_loads(k.k, k.nrec, kbuf, offs_k(t));
-        }
-        if (!with_v) return;
-        if (t - 1 < TP) Cd::load(codes_v, v.v, v.nrec, slot0, l);
-        else issue_loads(v.v, v.nrec, vbuf, offs_v(t - 1));
-    };
-    auto store_codes = [&](int t, bool with_v, char *kbuf, char *vbuf) __attribute__((always_inline)) {
-        if (t < TP) Cd::template store<false>(codes_k, scales_k, kbuf, w, l);
-        if (with_v && t - 1 < TP) Cd::template store<true>(codes_v, scales_v, vbuf, w, l);
+    auto request_k = [&](const auto &src, int t) __attribute__((always_inline)) {      // (past the last tile: no bytes)
         scales_v = scales_k;
+        const int bytes = t < n_tiles ? src.nrec : 0;
+        Cd::load(codes_k, src.k, bytes, slot0, l);
+        if constexpr (KV8) Cd::load_scales(scales_k, src.scales, bytes, slot0, l);
+    };
+    auto request_v = [&](const auto &src, int t) __attribute__((always_inline)) { Cd::load(codes_v, src.v, t < n_tiles ? src.nrec : 0, slot0, l); };
+    // K tile t and V tile t - 1: asked for, brought to LDS
+    auto request = [&](const auto &k, const auto &v, int t) __attribute__((always_inline)) {
+        if (t < TP) request_k(k, t);
+        else scales_v = scales_k;
+        if (t - 1 < TP) request_v(v, t - 1);
+    };
+    auto direct = [&](const auto &k, const auto &v, int t, char *kbuf, char *vbuf) __attribute__((always_inline)) {
+        if (t >= TP) issue_loads(k.k, k.nrec, kbuf, offs_k(t));
+        if (t - 1 >= TP) issue_loads(v.v, v.nrec, vbuf, offs_v(t - 1));
+    };
+    auto store_codes = [&](int t, char *kbuf, char *vbuf) __attribute__((always_inline)) {
+        if (t < TP) Cd::template store_all<false>(codes_k, scales_k, kbuf, w, l);
+        if (t - 1 < TP) Cd::template store_all<true>(codes_v, scales_v, vbuf, w, l);
     };
 
     // ---- running state of the two sub-tiles ----
@@ -1187,6 +1297,8 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
     for (int s = 0; s < 2; s++)
 #pragma unroll
         for (int r = 0; r < 16; r++) negM[s][r] = 0.f;
+    // (8-bit pools: the reference, and the largest row sum of a block that leaves it where it is; see the kernel above)
+    [[maybe_unused]] float ref[2] = {0.f, 0.f}, lb_max[2] = {-1.f, -1.f};
 
     int k_off[Gm::DC];
 #pragma unroll
@@ -1224,8 +1336,12 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
     // ---- prologue ----
     Src prev = tile_src(0);
     if constexpr (KV8) {
-        fetch_codes(prev, prev, 0, false, sK0, nullptr);
-        store_codes(0, false, sK0, nullptr);
+        if (TP > 0) {
+            request_k(prev, 0);
+            Cd::template store_all<false>(codes_k, scales_k, sK0, w, l);
+        } else {
+            issue_loads(prev.k, prev.nrec, sK0, offs_k(0));
+        }
     } else {
         issue_loads(prev.k, prev.nrec, sK0, offs_k(0));
     }
@@ -1251,10 +1367,10 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
     ones[0] = (__bf16)1.0f;
     ones[1] = (__bf16)1.0f;
 
-    auto exp_pair = [&](const f32x16 &Tc, bf16x8 (&Pc)[2], float &lbs, int r) __attribute__((always_inline)) {
+    auto exp_pair = [&](int s, const f32x16 &Tc, bf16x8 (&Pc)[2], float &lbs, int r) __attribute__((always_inline)) {
         f32x2 pv;
-        pv[0] = __builtin_amdgcn_exp2f(Tc[r]);
-        pv[1] = __builtin_amdgcn_exp2f(Tc[r + 1]);
+        pv[0] = __builtin_amdgcn_exp2f(KV8 ? fmaf(Tc[r], c, -ref[s]) : Tc[r]);
+        pv[1] = __builtin_amdgcn_exp2f(KV8 ? fmaf(Tc[r + 1], c, -ref[s]) : Tc[r + 1]);
         const bf16x2 pk = __builtin_convertvector(pv, bf16x2);
         Pc[r / 8][r % 8] = pk[0];
         Pc[r / 8][r % 8 + 1] = pk[1];
@@ -1280,6 +1396,13 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
         t[(r % 8) / 2] = bits;
         Pc[r / 8] = __builtin_bit_cast(bf16x8, t);
     };
+    // a group's packed probabilities r .. to their place
+    auto put_bits = [&](const int (&bits)[2], bf16x8 (&Pc)[2], int r) __attribute__((always_inline)) {
+        i32x4 t = __builtin_bit_cast(i32x4, Pc[r / 8]);
+        t[(r % 8) / 2] = bits[0];
+        if constexpr (H == 4) t[(r % 8) / 2 + 1] = bits[1];
+        Pc[r / 8] = __builtin_bit_cast(bf16x8, t);
+    };
     // Row sums of a finished block of both sub-tiles, from its packed (rounded) probabilities, in
     // score order: the same dot2 chain as the other forms of the kernel run.  A dot2 goes through the
     // matrix pipe in order with the MFMAs, so the sixteen stand together, at the start of the
@@ -1297,23 +1420,35 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
             }
         }
     };
+    auto line = [&](int s) __attribute__((always_inline)) { return KV8 ? lb_max[s] : RESCALE_SUM; };
     // the reference move of one sub-tile (see the kernel above); its scores and outputs have settled
     auto redo_block = [&](int s, f32x16 &Tc, f32x16 &Tn, bf16x8 (&Pp)[2], bool first_check) __attribute__((always_inline)) {
         float mxp = Tn[0];
 #pragma unroll
         for (int r = 1; r < 16; r++) mxp = fmaxf(mxp, Tn[r]);
         mxp = xmax32(mxp);
-        const float d = first_check ? mxp : fmaxf(mxp, 0.f);
-        const float alpha = first_check ? 1.f : __builtin_amdgcn_exp2f(-d);
+        bool first = first_check, none = false;
+        if constexpr (KV8) {
+            mxp = fmaf(mxp, c, -ref[s]);
+            first = xsum32(l_part[s]) == 0.f;                     // nothing of this row has counted so far
+            none = first && mxp == -INFINITY;
+            lb_max[s] = __any(none) ? -1.f : RESCALE_SUM;
+        }
+        const float d = none ? 0.f : first ? mxp : fmaxf(mxp, 0.f);
+        const float alpha = first ? 1.f : __builtin_amdgcn_exp2f(-d);
         l_part[s] *= alpha;
 #pragma unroll
         for (int db = 0; db < Gm::DB; db++) O[s][db] *= alpha;
-        Tn -= d;
-        Tc -= d;
-        negM[s] -= d;
+        if constexpr (KV8) {
+            ref[s] += d;
+        } else {
+            Tn -= d;
+            Tc -= d;
+            negM[s] -= d;
+        }
         lb[s] = 0.f;
 #pragma unroll
-        for (int r = 0; r < 16; r += 2) exp_pair(Tn, Pp, lb[s], r);
+        for (int r = 0; r < 16; r += 2) exp_pair(s, Tn, Pp, lb[s], r);
     };
     auto redo_both = [&](f32x16 (&Tc)[2], f32x16 (&Tn)[2], bf16x8 (&Pp)[2][2], bool first_check) __attribute__((always_inline)) {
         SETTLE_V2(Tn[0], Tn[1]);
@@ -1321,10 +1456,10 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
 #pragma unroll
         for (int db = 0; db < Gm::DB; db++) SETTLE_A2(O[0][db], O[1][db]);
         // each sub-tile moves its reference exactly when a wave serving it alone would
-        const bool r0 = __any(!(lb[0] <= RESCALE_SUM)), r1 = __any(!(lb[1] <= RESCALE_SUM));
-        if (first_check || r0) redo_block(0, Tc[0], Tn[0], Pp[0], first_check);
-        if (first_check || r1) redo_block(1, Tc[1], Tn[1], Pp[1], first_check);
-        SETTLE_V2(negM[0], negM[1]);
+        const bool r0 = __any(!(lb[0] <= line(0))), r1 = __any(!(lb[1] <= line(1)));
+        if ((!KV8 && first_check) || r0) redo_block(0, Tc[0], Tn[0], Pp[0], first_check);
+        if ((!KV8 && first_check) || r1) redo_block(1, Tc[1], Tn[1], Pp[1], first_check);
+        if constexpr (!KV8) SETTLE_V2(negM[0], negM[1]);
 #pragma unroll
         for (int db = 0; db < Gm::DB; db++) SETTLE_A2(O[0][db], O[1][db]);
     };
@@ -1337,19 +1472,20 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
     // next step will fetch is worked out in the middle of this one.
     i32x4 op[PFW + 1];
     Src pre = prev;                                        // source of tile j + 1 while step j runs
-    auto step = [&](int j, char *kcur, char *knext, char *vprev, char *vcur) __attribute__((always_inline)) {
+    auto step = [&](auto codes, int j, char *kcur, char *knext, char *vprev, char *vcur) __attribute__((always_inline)) {
+        constexpr bool CODES = decltype(codes)::value != 0;
         constexpr int NM = 4 * H;
         constexpr int NL = 2 * Gm::NI;                     // tile loads of the step, one per group of its first half
         static_assert(NL <= H, "the tile loads of a step fit its first half iteration");
         static_assert(NM % (PFW + 1) == 0 && PFW <= H, "the operand ring closes at the step boundary");
         const Src next = pre;
         const Offs ok = offs_k(j + 1), ov = offs_v(j);
-        const bool masked = j >= TPF;
+        const bool masked = !CODES && j >= TPF;
         const auto rsrc_k = __builtin_amdgcn_make_buffer_rsrc((void *)next.k, 0, next.nrec, RSRC_FLAGS);
         const auto rsrc_v = __builtin_amdgcn_make_buffer_rsrc((void *)prev.v, 0, prev.nrec, RSRC_FLAGS);
         lds_void *dst_k = (lds_void *)(knext + w * Gm::RW * ROWB);
         lds_void *dst_v = (lds_void *)(vcur + w * Gm::RW * ROWB);
-        if constexpr (KV8) fetch_codes(next, prev, j + 1, true, knext, vcur);
+        if constexpr (KV8 && !CODES) direct(next, prev, j + 1, knext, vcur);
         prev = next;
 
         auto operand = [&](auto mc) {
@@ -1366,8 +1502,13 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
             if constexpr (m + PFW == NM) {
                 // every LDS read of this step's tiles has been issued; once they have returned and this
                 // wave's part of the fetched tiles has landed, the waves meet
-                if constexpr (KV8) store_codes(j + 1, true, knext, vcur);
-                __builtin_amdgcn_s_waitcnt(0x0070);           // vmcnt(0) lgkmcnt(0)
+                if constexpr (CODES) {
+                    __builtin_amdgcn_s_waitcnt(0xC07F);       // lgkmcnt(0): the loads in flight are the next step's
+                } else {
+                    if constexpr (KV8) store_codes(j + 1, knext, vcur);
+                    __builtin_amdgcn_s_waitcnt(0x0070);       // vmcnt(0) lgkmcnt(0)
+                    if constexpr (KV8) request(pre, next, j + 2);
+                }
                 __syncthreads();
             }
             op[(m + PFW) % (PFW + 1)] = operand(IntC<m + PFW>{});
@@ -1378,7 +1519,7 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
             constexpr int m0 = i * 2 * H;
             constexpr int PPG = 8 / H;                     // score pairs exponentiated beside one operand's two MFMAs
             block_sums(Pp);
-            if (__builtin_expect(first_check || __any(!(lb[0] <= RESCALE_SUM) || !(lb[1] <= RESCALE_SUM)), 0)) redo_both(Tc, Tn, Pp, first_check);
+            if (__builtin_expect((!KV8 && first_check) || __any(!(lb[0] <= line(0)) || !(lb[1] <= line(1))), 0)) redo_both(Tc, Tn, Pp, first_check);
             l_part[0] += lb[0];
             l_part[1] += lb[1];
             lb[0] = 0.f;
@@ -1390,6 +1531,12 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
             static_for([&](auto sc) {
                 constexpr int s2 = decltype(sc)::value, m = m0 + s2;
                 fetch(IntC<m>{});
+                if constexpr (KV8) {
+                    int bits[2];
+                    kv8_group_s<PPG>(s2 == 0, Tn, op[m % (PFW + 1)], qreg[0][s2], qreg[1][s2], Tc[0], 2 * PPG * s2, c, ref[0], bits);
+                    __builtin_amdgcn_sched_barrier(0);
+                    put_bits(bits, Pc[0], 2 * PPG * s2);
+                } else {
                 f32x2 pv[PPG];
                 if constexpr (s2 == 0) s_first(Tn[0], op[m % (PFW + 1)], qreg[0][s2], negM[0]);
                 else s_acc(Tn[0], op[m % (PFW + 1)], qreg[0][s2]);
@@ -1405,6 +1552,17 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
                     else __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_v, dst_v, 16, ov.v[li2], 0, li2 * 1024, 0);
                 }
                 static_for([&](auto pc) { exp_pair_b(pv[pc.value], Pc[0], 2 * (PPG * s2 + pc.value)); }, std::make_integer_sequence<int, PPG>{});
+                }
+                if constexpr (CODES && i == 1) {
+                    // eight codes a group: K's, then V's, then the next step's are asked for
+                    static_assert(2 * Cd::CHUNKS == H, "one of a group's each");
+                    if constexpr (s2 < Cd::CHUNKS) Cd::template store<false>(codes_k, scales_k, knext, w, l, s2);
+                    else Cd::template store<true>(codes_v, scales_v, vcur, w, l, s2 - Cd::CHUNKS);
+                    if constexpr (s2 == H - 1) {
+                        request_k(pre, j + 2);
+                        request_v(next, j + 1);
+                    }
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }, std::make_integer_sequence<int, H>{});
             if (__builtin_expect(masked, 0)) {
@@ -1421,6 +1579,12 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
             static_for([&](auto sc) {
                 constexpr int s2 = decltype(sc)::value, m = m0 + H + s2;
                 fetch(IntC<m>{});
+                if constexpr (KV8) {
+                    int bits[2];
+                    kv8_group_o<PPG>(O[0][s2 % Gm::DB], O[1][s2 % Gm::DB], op[m % (PFW + 1)], as_i(Pp[0][s2 / Gm::DB]), as_i(Pp[1][s2 / Gm::DB]), Tc[1], 2 * PPG * s2, c, ref[1], bits);
+                    __builtin_amdgcn_sched_barrier(0);
+                    put_bits(bits, Pc[1], 2 * PPG * s2);
+                } else {
                 f32x2 pv[PPG];
                 mfma_o_acc(O[0][s2 % Gm::DB], op[m % (PFW + 1)], as_i(Pp[0][s2 / Gm::DB]));
                 __builtin_amdgcn_sched_barrier(0);
@@ -1429,6 +1593,7 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
                 mfma_o_acc(O[1][s2 % Gm::DB], op[m % (PFW + 1)], as_i(Pp[1][s2 / Gm::DB]));
                 __builtin_amdgcn_sched_barrier(0);
                 static_for([&](auto pc) { exp_pair_b(pv[pc.value], Pc[1], 2 * (PPG * s2 + pc.value)); }, std::make_integer_sequence<int, PPG>{});
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }, std::make_integer_sequence<int, H>{});
         };
@@ -1439,14 +1604,14 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
     {
         const Src next = tile_src(1);
         if constexpr (KV8) {
-            fetch_codes(next, prev, 1, true, sK1, sV0);
+            request(next, prev, 1);
+            direct(next, prev, 1, sK1, sV0);
         } else {
             issue_loads(next.k, next.nrec, sK1, offs_k(1));
             issue_loads(prev.v, prev.nrec, sV0, offs_v(0));
         }
         prev = next;
         pre = tile_src(2);
-        if constexpr (KV8) asm volatile("s_nop 1" : "+v"(negM[0]), "+v"(negM[1]));      // (their zeros are written)
         static_for([&](auto dc) {
             const i32x4 a0 = k_operand(sK0, 0, dc.value), a1 = k_operand(sK0, 1, dc.value);
             if constexpr (dc.value == 0) {
@@ -1470,21 +1635,34 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
                 if (needs_mask(0, 1, s)) mask_block(T1[s], 0, 1, s);
             }
         }
-        if constexpr (KV8) store_codes(1, true, sK1, sV0);
+        if constexpr (KV8) store_codes(1, sK1, sV0);
         __builtin_amdgcn_s_waitcnt(0x0F70);
+        if constexpr (KV8) request(pre, prev, 2);
         __syncthreads();
         static_for([&](auto mc) { op[mc.value] = k_operand(sK1, 0, mc.value); }, std::make_integer_sequence<int, PFW>{});
     }
-    for (int j = 1; j < n_tiles; j += 2) {
-        step(j, sK1, sK0, sV0, sV1);
-        if (j + 1 < n_tiles) step(j + 1, sK0, sK1, sV1, sV0);
+    int first = 1;
+    if constexpr (KV8) {
+        for (; first + 3 < TP; first += 2) {               // (what both steps ask for lies in the prefix, too)
+            step(IntC<1>{}, first, sK1, sK0, sV0, sV1);
+            step(IntC<1>{}, first + 1, sK0, sK1, sV1, sV0);
+        }
+        // the other loop holds O in other registers: it is moved once the last products are there
+        if constexpr (D == 128)
+            asm volatile("s_nop 15\n\ts_nop 3" : "+a"(O[0][0]), "+a"(O[0][1]), "+a"(O[0][2]), "+a"(O[0][3]), "+a"(O[1][0]), "+a"(O[1][1]), "+a"(O[1][2]), "+a"(O[1][3]));
+        else
+            asm volatile("s_nop 15\n\ts_nop 3" : "+a"(O[0][0]), "+a"(O[0][1]), "+a"(O[1][0]), "+a"(O[1][1]));
+    }
+    for (int j = first; j < n_tiles; j += 2) {
+        step(IntC<0>{}, j, sK1, sK0, sV0, sV1);
+        if (j + 1 < n_tiles) step(IntC<0>{}, j + 1, sK0, sK1, sV1, sV0);
     }
     // drain: probabilities of the last block, products of tile n_tiles - 1
     {
         const char *vlast = (n_tiles - 1) & 1 ? sV1 : sV0;
         auto exp_all = [&](int s, f32x16 &Tc, bf16x8 (&Pc)[2]) __attribute__((always_inline)) {
 #pragma unroll
-            for (int r = 0; r < 16; r += 2) exp_pair(Tc, Pc, lb[s], r);
+            for (int r = 0; r < 16; r += 2) exp_pair(s, Tc, Pc, lb[s], r);
         };
         auto product = [&](int kb, bf16x8 (&Pp)[2][2]) __attribute__((always_inline)) {
             static_for([&](auto sc) {
@@ -1495,7 +1673,7 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
             }, std::make_integer_sequence<int, H>{});
         };
         block_sums(P0);
-        if (n_tiles == 1 || __any(!(lb[0] <= RESCALE_SUM) || !(lb[1] <= RESCALE_SUM))) redo_both(T1, T0, P0, n_tiles == 1);
+        if ((!KV8 && n_tiles == 1) || __any(!(lb[0] <= line(0)) || !(lb[1] <= line(1)))) redo_both(T1, T0, P0, n_tiles == 1);
         l_part[0] += lb[0];
         l_part[1] += lb[1];
         lb[0] = 0.f;
@@ -1504,7 +1682,7 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
         exp_all(0, T1[0], P1[0]);
         exp_all(1, T1[1], P1[1]);
         product(0, P0);
-        if (__any(!(lb[0] <= RESCALE_SUM) || !(lb[1] <= RESCALE_SUM))) redo_both(T0, T1, P1, false);
+        if (__any(!(lb[0] <= line(0)) || !(lb[1] <= line(1)))) redo_both(T0, T1, P1, false);
         l_part[0] += lb[0];
         l_part[1] += lb[1];
         product(1, P1);
