@@ -20,7 +20,10 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) short i16x2;
 typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
 
-constexpr int KV8_MAX_WGS = 2048;   // 8 work-groups of 4 waves per CU
+// Work-groups of a launch: one per part, where the copy kernels of plain rows hold a grid of the chip's size that strides over them.  A work-group has one trip's
+// loads and is gone; the dispatcher evens out what a second, half empty round leaves idle.  us, 2048 and one per part: append of 32768 tokens of 8 heads of
+// 128 40.3, 37.2; read of as many 48.1, 40.3, of 12001 17.8, 16.6.
+constexpr int KV8_MAX_WGS = 1 << 20;
 
 #if defined(__HIP_DEVICE_COMPILE__)
 static __device__ __forceinline__ int clamp_page(int pg, int num_pages) {
@@ -106,7 +109,7 @@ static __device__ __forceinline__ Row16 values(const u32x4 &codes, float scale) 
 #endif
 
 // Work: runs of up to 16 tokens of one request in one page, cut into parts of 256 items; an item's number counts lanes of a row, heads, tokens,
-// in the packed rows' order.  A grid sized to the chip strides over (run, part).
+// in the packed rows' order.
 template <int D, bool READ>
 __global__ __launch_bounds__(256) void kv8_copy_kernel(AppendParams p, unsigned parts_per_run, int step_runs, unsigned step_parts) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -132,7 +135,9 @@ __global__ __launch_bounds__(256) void kv8_copy_kernel(AppendParams p, unsigned 
         uint16_t *sc = (uint16_t *)(page + codes_bytes) + g * 16 + slot;
         u32x4 *kp = (u32x4 *)p.k_new + packed, *vp = (u32x4 *)p.v_new + packed;
         if constexpr (READ) {
-            const u32x4 k = *kc, v = *vc;
+            // d = 128: a row is a line, read once.  At 64 the neighbour's row shares it and comes with another wave: under the streaming hint it
+            // is fetched twice (16 requests of up to 4096 tokens, 2 heads of 64: 5.1 and 6.1 us; 32768 tokens of 8 of 128: 47.6 without the hint, 40.3 with)
+            const u32x4 k = D == 128 ? __builtin_nontemporal_load(kc) : *kc, v = D == 128 ? __builtin_nontemporal_load(vc) : *vc;
             const unsigned s = *sc;
             const Row16 x = values(k, __uint_as_float((s & 0xff) << 23)), y = values(v, __uint_as_float((s >> 8) << 23));
             __builtin_nontemporal_store(x.a, kp);
