@@ -74,7 +74,8 @@ typedef enum {
     PBKV_ERR_DEVICE = -6,  /* HIP runtime error, or a pointer of the wrong kind   */
     PBKV_ERR_LIMIT = -7    /* the call needs more descriptor space than the library
                               can provide at once, or the pool is 1 TiB (8-bit:
-                              512 GiB) or more                                    */
+                              512 GiB) or more, or a page is 2 GiB or more (8-bit
+                              pools, and pbkv_read_kv)                            */
 } pbkv_status;
 
 /* PBKV_BF16_KV8: q, k_new, v_new and out are bf16, the pool holds 8-bit rows (see "8-bit pool" below). */
@@ -97,13 +98,14 @@ typedef struct {
  *     e    = the smallest exponent with which the row's largest finite magnitude is at most 448 * 2^e, within [-111, 119];  b = e + 127
  *     code = x * 2^-e rounded to the nearest e4m3 number, ties to even; above 448 * 2^119 it saturates; infinities and NaN become NaN
  * so a value is off by at most 2^-4 of itself, or by 2^(e - 10) where it is below 2^(e - 6).  The values are bf16 numbers
- * without further rounding: attention over the pool computes what it would over a bf16 pool that holds them.  A page is one contiguous
- * block of pbkv_page_bytes() bytes, which the swaps move as they are:
+ * without further rounding, and attention over the pool is what it would be over a bf16 pool that holds them, up to rounding.  A page is one
+ * contiguous block of pbkv_page_bytes() bytes, which the swaps move as they are:
  *     codes  [2][num_kv_heads][page_size][head_dim]   (index 0 = K, 1 = V)
  *     scales [num_kv_heads][page_size][2]             (K, V)
  *     nothing up to a multiple of 128 bytes           (never written, never read)
- * Scale bytes have to be in 16 .. 246, as append leaves them, in every slot that a call reads as a token.  In all calls the same
- * limits hold as for PBKV_BF16, but for the pool's size, which is less than 512 GiB.
+ * Scale bytes have to be in 16 .. 246, as append leaves them, in every slot that a call reads as a token.  Other slots may hold
+ * anything.  A row with a NaN makes the results that depend on it NaN.  In all calls the same limits hold as for PBKV_BF16, but for the
+ * pool's size, which is less than 512 GiB, and a page's, less than 2 GiB.
  */
 
 /* Bytes of one pool page for this shape: 2 * H_kv * P * d * element size, or 2 * H_kv * P * (d + 1) rounded up to a multiple of 128
@@ -124,7 +126,8 @@ int64_t pbkv_page_bytes(const pbkv_shape *shape);
  *   q, k_new, v_new, kv_pool, block_table : device, read only
  *   prefix_lens, new_lens                 : host int32 [batch], read during the call
  *   out                                   : device, written; rows of other calls untouched
- * With an 8-bit pool the prefix is the values that the pool holds; the suffix, k_new and v_new, is not quantised.
+ * With an 8-bit pool the prefix is the values that the pool holds; the suffix, k_new and v_new, is not quantised.  Q is not rounded then
+ * (with a bf16 pool once more, after its scaling).
  * bf16: fp32 accumulation, probabilities rounded to bf16 before the PV product, one
  * final rounding to bf16.  f32: fp32 throughout.
  * A call repeated on the same inputs gives the same bits (unless memory for partial results runs out in

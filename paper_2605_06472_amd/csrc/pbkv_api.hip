@@ -68,6 +68,7 @@ int check_shape(const pbkv_shape *s, bool need_heads) {
     const int top = s->dtype == PBKV_BF16_KV8 ? 39 : 40;
     if ((int64_t)s->num_pages * page_bytes(s) >= (int64_t)1 << top)
         return fail(PBKV_ERR_LIMIT, "pool of %d pages is %s or more", s->num_pages, top == 39 ? "512 GiB" : "1 TiB");
+    if (s->dtype == PBKV_BF16_KV8 && page_bytes(s) > INT32_MAX) return fail(PBKV_ERR_LIMIT, "a page of %d KV heads is 2 GiB or more", s->num_kv_heads);
     if (need_heads) {
         if (s->num_q_heads <= 0 || s->num_q_heads % s->num_kv_heads != 0)
             return fail(PBKV_ERR_SHAPE, "num_q_heads %d is not a multiple of num_kv_heads %d",
@@ -1044,6 +1045,7 @@ int move_kv(const pbkv_shape *s, void *k_new, void *v_new, void *kv_pool, const 
     int64_t N = 0;
     if ((rc = check_lens(s, prefix_lens, new_lens, &N))) return rc;
     if (N == 0) return PBKV_OK;
+    if (read && page_bytes(s) > INT32_MAX) return fail(PBKV_ERR_LIMIT, "%s: a page of %d KV heads is 2 GiB or more", who, s->num_kv_heads);
     if ((rc = check_aligned(k_new, read ? "k" : "k_new")) || (rc = check_aligned(v_new, read ? "v" : "v_new")) ||
         (rc = check_aligned(kv_pool, "kv_pool")))
         return rc;

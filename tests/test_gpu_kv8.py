@@ -158,6 +158,22 @@ def test_decode_of_larger_batches(oracle, heads, batch, ctx):
     assert torch.equal(d.decode(), got)
 
 
+def test_decode_slices_of_more_pages_than_a_wave_holds_ids_for(oracle):
+    """A call so large that its contexts stay in slices of a thousand pages: many requests over the same pages, in two orders."""
+    hkv, d, pages, ctx, batch = 8, 128, 1000, 15997, 280
+    b = small(251, (32, 8, 128), prefix_lens=(ctx, ctx), new_lens=(1, 1), num_pages=2 * pages + 2)
+    kb = make(b)
+    want = oracle.decode(b.q, kb.values, b.block_table, b.prefix_lens)
+    table = to_torch(b.block_table).repeat(batch // 2, 1).contiguous()
+    q = to_torch(b.q).repeat(batch // 2, 1, 1).contiguous()
+    shape = binding.make_shape(batch, 32, hkv, d, 16, b.num_pages, b.max_pages, "bf16_kv8")
+    out = torch.full_like(q, 7.0)
+    binding.paged_decode(shape, q, torch.from_numpy(kb.pool).cuda(), table, np.full(batch, ctx, np.int32), out)
+    got = f64(out).reshape(batch // 2, 2, 32, d)
+    assert (got == got[:1]).all()
+    decode_close(got[0], want, b, kb.values, (ctx,), "decode")
+
+
 def test_decode_over_scales_of_every_size(oracle):
     """Keys and values whose rows lie far apart in magnitude, and a maximum that comes late."""
     b = small(250, (8, 2, 128), prefix_lens=(700, 33, 1200), new_lens=(1,) * 3, num_pages=160)
@@ -266,6 +282,31 @@ def test_an_infinity_shows():
         binding.paged_decode(d.shape, d.q[:3], d.pool, d.block_table, b.prefix_lens, one)
         assert bool(torch.isnan(one[1, 4:] if kv == 0 else one[1, 4:, 77]).all()) and bool(torch.isfinite(one[[0, 2]]).all())
         assert bool(torch.isfinite(one[1, :4]).all())
+
+
+def test_rows_of_q_two_gib_apart(oracle):
+    """So many heads that tokens of a wave lie 2 GiB apart in q: the form that reaches them."""
+    heads, d, n, p = 262144, 128, 33, 20
+    g = torch.Generator(device="cuda").manual_seed(9)
+    rnd = lambda *s: torch.empty(s, dtype=torch.bfloat16, device="cuda").normal_(0, 0.5, generator=g)      # noqa: E731
+    shape = binding.make_shape(1, heads, heads, d, 16, 4, 4, "bf16_kv8")
+    pool = torch.zeros((4, K8.page_bytes(heads, d)), dtype=torch.uint8, device="cuda")
+    table = torch.tensor([[2, 0, 3, 1]], dtype=torch.int32, device="cuda")
+    zero, pre, new = np.array([0], np.int32), np.array([p], np.int32), np.array([n], np.int32)
+    k0, v0 = rnd(p, heads, d), rnd(p, heads, d)
+    binding.append_kv(shape, k0, v0, pool, table, zero, pre)
+    k, v = torch.zeros_like(k0), torch.zeros_like(v0)
+    binding.read_kv(shape, pool, table, zero, pre, k, v)
+    q, k_new, v_new = rnd(n, heads, d), rnd(n, heads, d), rnd(n, heads, d)
+    out = torch.full_like(q, 7.0)
+    binding.prefix_prefill(shape, q, k_new, v_new, pool, table, pre, new, out)
+    torch.cuda.synchronize()
+    for h in (0, 1, heads // 2 + 3, heads - 1):
+        assert (k[:, h].float() - k0[:, h].float()).abs().max() <= 2.0 ** -4 * k0[:, h].float().abs().max()
+        keys, vals = (torch.cat((a[:, h], c[:, h])).double() for a, c in ((k, k_new), (v, v_new)))
+        s = q[:, h].double() @ keys.T / d ** 0.5
+        s.masked_fill_(torch.arange(p + n, device="cuda") > p + torch.arange(n, device="cuda")[:, None], -float("inf"))
+        prefill_close(f64(out[:, h]), (torch.softmax(s, -1) @ vals).cpu().numpy(), "head %d" % h)
 
 
 # ---- as a server uses them ------------------------------------------------------------------------------------------

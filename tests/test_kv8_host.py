@@ -61,6 +61,11 @@ def test_what_else_is_refused():
     pages = (1 << 39) // 33024
     assert _code(_read, _shape(num_pages=pages, dtype="bf16_kv8"), [0], [16]) == -6
     assert _code(_read, _shape(num_pages=pages + 1, dtype="bf16_kv8"), [0], [16]) == -7
+    # the largest page: 2 GiB
+    heads = (1 << 31) // (32 * 129)
+    assert _code(_read, _shape(num_q_heads=heads, num_kv_heads=heads, num_pages=1, dtype="bf16_kv8"), [0], [16]) == -6
+    assert _code(_read, _shape(num_q_heads=heads + 1, num_kv_heads=heads + 1, num_pages=1, dtype="bf16_kv8"), [0], [16]) == -7
+    assert _code(_read, _shape(num_q_heads=1 << 18, num_kv_heads=1 << 18, num_pages=1), [0], [16]) == -7
 
 
 # ---- over the recording runtime ----------------------------------------------------------------------------------
