@@ -9,11 +9,15 @@
 //              of the contraction, so a lane takes 16 codes with one load (d = 64 j + 16 g ..) and feeds two MFMAs with them, Q^T
 //              being loaded in the same order.  Codes become bf16 exactly, two per instruction, without their scale: that
 //              multiplies the token's score, of which a lane has four, and not its 8 d.
-//   P V        up to four heads as in the bf16 kernel, in fp32 on the 4x4x1 MFMA; a V code becomes fp32 with its scale in the conversion,
-//              two per instruction, where bf16 took one each.  8 and 16 heads on the 16x16x16 bf16 MFMA, which takes the page's
-//              16 tokens at once: V codes are bf16 numbers, and a probability (times its token's scale) goes in as two, the nearest and
-//              what that leaves, 16 bits in all (an error of 2^-17 of it where the result is rounded to 2^-8).  The fp32 forms take four and two
-//              times the matrix pipe's clocks.  Both scales of a lane's four tokens are one 8-byte load.
+//   P V        on the 16x16x16 bf16 MFMA, which takes the page's 16 tokens at once: V codes are bf16 numbers, and a probability (times its
+//              token's scale) goes in as two, the nearest and what that leaves, 16 bits in all -- an error of 2^-17 of it, where the result
+//              is rounded to 2^-8.  Against the bf16 kernel's fp32 forms that is as fast up to 4 heads (201 us both for 64 requests of 1024 ..
+//              16384 tokens at 32/8 heads of 128), whose 4x4x1 products take as many clocks, and faster past it: 62.4 -> 58.1 at 16/2, 80.4 -> 62.9 at
+//              32/2, 36.0 -> 32.3 at 16/2 of 64.  A lane holds d E c .. of four tokens, a word each: four by four bytes are transposed, so that a word is
+//              four tokens of one d.  Both scales of its tokens are one 8-byte load.
+//   loads      5.8 TB/s of codes at 64 requests of 1024 .. 16384 tokens at 32/8 heads of 128.  What a page's rows take without any arithmetic is
+//              197 us of the 201 there; scales, whose line serves four heads on four XCDs, 4 of them.  K rows are read in two halves, which the streaming hint
+//              would fetch twice (215 -> 202).
 #include "decode_common.h"
 
 #include <algorithm>
@@ -33,28 +37,18 @@ static __device__ __forceinline__ unsigned word(const u32x2 &v, int i) { return 
 static __device__ __forceinline__ unsigned word(unsigned v, int) { return v; }
 
 // A wave's result to LDS (rows padded by 16 bytes: the lanes of a 16-lane group store 16 bytes to a row each).
-template <int D, int HB>
+template <int D>
 static __device__ __forceinline__ void leave_wave(const f32x4 (&acc)[D / 16], float M, float lsum, int G, float *part, float *part_m, float *part_l) {
     constexpr int E = D / 16, PR = D + 4;
     const int g = (threadIdx.x & 63) >> 4, c = threadIdx.x & 15;
     lsum = fold16(lsum, lsum);
     lsum = fold32(lsum, lsum);
-    if constexpr (HB == 0) {
-        if (c < G) {
-            float *ps = part + c * PR + 4 * g * E;
+    if (c < G) {
+        float *ps = part + c * PR + 4 * g * E;
 #pragma unroll
-            for (int q = 0; q < 4; q++)
+        for (int q = 0; q < 4; q++)
 #pragma unroll
-                for (int e = 0; e < E; e += 4) *(f32x4 *)(ps + q * E + e) = f32x4{acc[e][q], acc[e + 1][q], acc[e + 2][q], acc[e + 3][q]};
-        }
-    } else {
-        // the four groups' shares: folded so that group g is left with head g
-        float o[E];
-#pragma unroll
-        for (int e = 0; e < E; e++) o[e] = fold16(fold32(acc[e][0], acc[e][2]), fold32(acc[e][1], acc[e][3]));
-        float *ps = part + g * PR + c * E;
-#pragma unroll
-        for (int e = 0; e < E; e += 4) *(f32x4 *)(ps + e) = f32x4{o[e], o[e + 1], o[e + 2], o[e + 3]};
+            for (int e = 0; e < E; e += 4) *(f32x4 *)(ps + q * E + e) = f32x4{acc[e][q], acc[e + 1][q], acc[e + 2][q], acc[e + 3][q]};
     }
     if (c < G && g == 0) {
         part_m[c] = M;
@@ -122,8 +116,8 @@ static __device__ __forceinline__ void finish_slice(const DecodeParams &p, const
 }
 
 
-// ARGUMENT: the list is `inl`, not in memory.  HB: the form of P V, 1 up to four query heads, 0 for 8 and 16.
-template <int D, bool FUSED, bool ARGUMENT, int HB>
+// ARGUMENT: the list is `inl`, not in memory.
+template <int D, bool FUSED, bool ARGUMENT>
 static __device__ __forceinline__ void decode_kv8_slice(const DecodeParams &p, const DecodeList &inl, int G) {
     constexpr int NK = D / 64;             // 16-byte K loads per page, each feeding two MFMAs
     constexpr int E = D / 16;              // d-values of a V row per lane
@@ -208,8 +202,7 @@ static __device__ __forceinline__ void decode_kv8_slice(const DecodeParams &p, c
     __shared__ __attribute__((aligned(16))) float part[DEC_WAVES][DEC_MAX_HEADS * PR];
     __shared__ float part_m[DEC_WAVES][DEC_MAX_HEADS], part_l[DEC_WAVES][DEC_MAX_HEADS];
 
-    // HB = 0: lane (g, c): acc[e][r] = O[d = E*(4g + r) + e][head c].  HB = 1: acc[e][r] = this lane's share, the tokens of
-    // its group g, of O[d = E*c + e][head r].  Reference and partial row sum of head c.
+    // lane (g, c): acc[e][r] = O[d = E*(4g + r) + e][head c]; reference and partial row sum of head c
     f32x4 acc[E];
 #pragma unroll
     for (int e = 0; e < E; e++) acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -257,13 +250,8 @@ static __device__ __forceinline__ void decode_kv8_slice(const DecodeParams &p, c
             lsum *= alpha;
 #pragma unroll
             for (int i = 0; i < 4; i++) t[i] = 4 * g + i < valid ? fmaf(s[i], ks[i], -M) : -INFINITY;
-            float al[4];
 #pragma unroll
-            for (int q = 0; q < 4; q++) al[q] = HB > 0 ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(alpha), q)) : alpha;
-#pragma unroll
-            for (int e = 0; e < E; e++)
-#pragma unroll
-                for (int q = 0; q < 4; q++) acc[e][q] *= al[q];
+            for (int e = 0; e < E; e++) acc[e] *= alpha;
         }
         float pr[4];
 #pragma unroll
@@ -280,40 +268,27 @@ static __device__ __forceinline__ void decode_kv8_slice(const DecodeParams &p, c
                     vs[i] = 1.f;
                 }
         }
-        if constexpr (HB == 1) {
+        bf16x4 hi, lo;
 #pragma unroll
-            for (int i = 0; i < 4; i++)
+        for (int i = 0; i < 4; i++) {
+            const float x = pr[i] * vs[i];
+            hi[i] = (__bf16)x;
+            lo[i] = (__bf16)(x - (float)hi[i]);
+        }
 #pragma unroll
-                for (int e = 0; e < E; e += 2) {
-                    const f32x2 v2 = e & 2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word(r.v[i], e / 4), vs[i], true)
-                                           : __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word(r.v[i], e / 4), vs[i], false);
-                    // (operand A: block 4g of each group of four blocks, lanes 16 g .., for all four of them)
+        for (int q = 0; q < E / 4; q++) {
+            // four tokens' words of four d each to four words of one d each
+            const unsigned a = word(r.v[0], q), b = word(r.v[1], q), c2 = word(r.v[2], q), d2 = word(r.v[3], q);
+            const unsigned ab0 = __builtin_amdgcn_perm(b, a, 0x05010400), ab1 = __builtin_amdgcn_perm(b, a, 0x07030602);
+            const unsigned cd0 = __builtin_amdgcn_perm(d2, c2, 0x05010400), cd1 = __builtin_amdgcn_perm(d2, c2, 0x07030602);
+            const unsigned t[4] = {__builtin_amdgcn_perm(cd0, ab0, 0x05040100), __builtin_amdgcn_perm(cd0, ab0, 0x07060302),
+                                   __builtin_amdgcn_perm(cd1, ab1, 0x05040100), __builtin_amdgcn_perm(cd1, ab1, 0x07060302)};
 #pragma unroll
-                    for (int x = 0; x < 2; x++) acc[e + x] = __builtin_amdgcn_mfma_f32_4x4x1f32(pr[i], v2[x], acc[e + x], 2, 0, 0);
-                }
-        } else {
-            bf16x4 hi, lo;
-#pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const float x = pr[i] * vs[i];
-                hi[i] = (__bf16)x;
-                lo[i] = (__bf16)(x - (float)hi[i]);
-            }
-#pragma unroll
-            for (int q = 0; q < E / 4; q++) {
-                // four tokens' words of four d each to four words of one d each
-                const unsigned a = word(r.v[0], q), b = word(r.v[1], q), c2 = word(r.v[2], q), d2 = word(r.v[3], q);
-                const unsigned ab0 = __builtin_amdgcn_perm(b, a, 0x05010400), ab1 = __builtin_amdgcn_perm(b, a, 0x07030602);
-                const unsigned cd0 = __builtin_amdgcn_perm(d2, c2, 0x05010400), cd1 = __builtin_amdgcn_perm(d2, c2, 0x07030602);
-                const unsigned t[4] = {__builtin_amdgcn_perm(cd0, ab0, 0x05040100), __builtin_amdgcn_perm(cd0, ab0, 0x07060302),
-                                       __builtin_amdgcn_perm(cd1, ab1, 0x05040100), __builtin_amdgcn_perm(cd1, ab1, 0x07060302)};
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    const bf16x2 v01 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(t[e], 1.f, false), v23 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(t[e], 1.f, true);
-                    const i16x4 v = __builtin_bit_cast(i16x4, __builtin_shufflevector(v01, v23, 0, 1, 2, 3));
-                    acc[4 * q + e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, __builtin_bit_cast(i16x4, hi), acc[4 * q + e], 0, 0, 0);
-                    acc[4 * q + e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, __builtin_bit_cast(i16x4, lo), acc[4 * q + e], 0, 0, 0);
-                }
+            for (int e = 0; e < 4; e++) {
+                const bf16x2 v01 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(t[e], 1.f, false), v23 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(t[e], 1.f, true);
+                const i16x4 v = __builtin_bit_cast(i16x4, __builtin_shufflevector(v01, v23, 0, 1, 2, 3));
+                acc[4 * q + e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, __builtin_bit_cast(i16x4, hi), acc[4 * q + e], 0, 0, 0);
+                acc[4 * q + e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v, __builtin_bit_cast(i16x4, lo), acc[4 * q + e], 0, 0, 0);
             }
         }
     };
@@ -336,29 +311,24 @@ static __device__ __forceinline__ void decode_kv8_slice(const DecodeParams &p, c
         }
     }
 done:
-    leave_wave<D, HB>(acc, M, lsum, G, part[w], part_m[w], part_l[w]);
+    leave_wave<D>(acc, M, lsum, G, part[w], part_m[w], part_l[w]);
     finish_slice<D, FUSED>(p, rq, req, kvh, slice, n_slices, G, part, part_m, part_l);
 }
 #endif
 
-template <int D, bool FUSED, bool ARGUMENT, int HB>
+template <int D, bool FUSED, bool ARGUMENT>
 __global__ __launch_bounds__(DEC_THREADS) __attribute__((amdgpu_waves_per_eu(D == 128 ? 2 : 4, D == 128 ? 2 : 4)))
 void decode_kv8_kernel(DecodeParams p, DecodeList inl, int G) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    decode_kv8_slice<D, FUSED, ARGUMENT, HB>(p, inl, G);
+    decode_kv8_slice<D, FUSED, ARGUMENT>(p, inl, G);
 #endif
-}
-
-template <int D, bool FUSED, bool ARGUMENT>
-static void (*kv8_kernel(int G))(DecodeParams, DecodeList, int) {
-    return G <= 4 ? decode_kv8_kernel<D, FUSED, ARGUMENT, 1> : decode_kv8_kernel<D, FUSED, ARGUMENT, 0>;
 }
 
 template <int D>
 static hipError_t launch_kv8(const DecodeParams &p, const DecodeList &inl, int G, hipStream_t s) {
     const dim3 grid((unsigned)p.n_slices * p.Hkv);
     const bool list = p.reqs == nullptr, fused = p.counters != nullptr;
-    auto kernel = fused ? (list ? kv8_kernel<D, true, true>(G) : kv8_kernel<D, true, false>(G)) : (list ? kv8_kernel<D, false, true>(G) : kv8_kernel<D, false, false>(G));
+    auto kernel = fused ? (list ? decode_kv8_kernel<D, true, true> : decode_kv8_kernel<D, true, false>) : (list ? decode_kv8_kernel<D, false, true> : decode_kv8_kernel<D, false, false>);
     hipLaunchKernelGGL(kernel, grid, dim3(DEC_THREADS), 0, s, p, inl, G);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || fused || p.n_slices == p.n_reqs) return e;          // every request is one slice
