@@ -9,20 +9,27 @@
 // two) does not depend on where in its range a row lies, and it is what makes the way back exact.
 //
 // Both are copies, bound by memory: 4 d bytes of bf16 per token and head on one side, 2 d + 2 on the other.  An item is 16 values of a row of
-// K and the same of V: two 16-byte loads of each in bf16, one 16-byte code word each, and both scales in one 16-bit
-// word, stored (or loaded) by the lanes of a row together.  The D / 16 lanes of a row find its largest magnitude by exchanges in the vector ALU.
+// K and the same of V, eight of each half of the row: so that the lanes of a row store and load 16-byte words of bf16, and 8-byte words of codes, side by side.
+// With 16 values in a run a store instruction writes every other 16 bytes, and streaming stores then reach memory in parts (1.28 times the
+// bytes that are there to write): 32768 tokens of 8 heads of 128, append 37.4 -> 32.5 us, read 39.7 -> 31.7 (6.4 TB/s; 4.9 is what a copy
+// of 2 GiB reaches); read of 12001 15.9 -> 10.6.  Both scales are one 16-bit word.  The D / 16 lanes of a row find its largest magnitude by exchanges in the
+// vector ALU.
+// Streaming hints where they were measured to pay: stores (append of 8 requests of 500 .. 1500 tokens 6.5 -> 5.5 us, of 32768 the same; read of 12001 12.9 ->
+// 10.6) and no load: a line of codes is read by two instructions (read 10.6, with the hint 15.4), and the rows to be appended are
+// best read as if their producer had just left them in a cache (append of 32768 35.5 with the hint, 32.5).
 #include "pbkv_internal.h"
 
 namespace pbkv {
 
 typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) short i16x2;
 typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
 
 // Work-groups of a launch: one per part, where the copy kernels of plain rows hold a grid of the chip's size that strides over them.  A work-group has one trip's
 // loads and is gone; the dispatcher evens out what a second, half empty round leaves idle.  us, 2048 and one per part: append of 32768 tokens of 8 heads of
-// 128 40.3, 37.2; read of as many 48.1, 40.3, of 12001 17.8, 16.6.
+// 128 33.0, 32.6, read 32.1, 31.7; of 2 requests of 3000 .. 5000 of 32 heads 32.0, 30.8 and 30.2, 29.6.
 constexpr int KV8_MAX_WGS = 1 << 20;
 
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -128,31 +135,29 @@ __global__ __launch_bounds__(256) void kv8_copy_kernel(AppendParams p, unsigned 
         const int c = idx % LPR;
         const unsigned row = (unsigned)idx / LPR, t = row / (unsigned)p.Hkv;
         const int g = (int)(row - t * p.Hkv), slot = d.slot0 + (int)t;
-        const int64_t packed = ((d.src_row + t) * p.Hkv + g) * (D / 8) + 2 * c;       // 16-byte words
+        const int64_t packed = ((d.src_row + t) * p.Hkv + g) * (D / 8) + c;           // 16-byte words
         char *page = (char *)p.kv_pool + (int64_t)clamp_page(page_id, p.num_pages) * page_bytes;
-        u32x4 *kc = (u32x4 *)(page + ((int64_t)g * 16 + slot) * D) + c;
-        u32x4 *vc = (u32x4 *)(page + ((int64_t)(p.Hkv + g) * 16 + slot) * D) + c;
+        u32x2 *kc = (u32x2 *)(page + ((int64_t)g * 16 + slot) * D) + c;
+        u32x2 *vc = (u32x2 *)(page + ((int64_t)(p.Hkv + g) * 16 + slot) * D) + c;
         uint16_t *sc = (uint16_t *)(page + codes_bytes) + g * 16 + slot;
         u32x4 *kp = (u32x4 *)p.k_new + packed, *vp = (u32x4 *)p.v_new + packed;
         if constexpr (READ) {
-            // d = 128: a row is a line, read once.  At 64 the neighbour's row shares it and comes with another wave: under the streaming hint it
-            // is fetched twice (16 requests of up to 4096 tokens, 2 heads of 64: 5.1 and 6.1 us; 32768 tokens of 8 of 128: 47.6 without the hint, 40.3 with)
-            const u32x4 k = D == 128 ? __builtin_nontemporal_load(kc) : *kc, v = D == 128 ? __builtin_nontemporal_load(vc) : *vc;
+            const u32x2 k0 = kc[0], k1 = kc[LPR], v0 = vc[0], v1 = vc[LPR];
             const unsigned s = *sc;
-            const Row16 x = values(k, __uint_as_float((s & 0xff) << 23)), y = values(v, __uint_as_float((s >> 8) << 23));
+            const Row16 x = values(u32x4{k0[0], k0[1], k1[0], k1[1]}, __uint_as_float((s & 0xff) << 23));
+            const Row16 y = values(u32x4{v0[0], v0[1], v1[0], v1[1]}, __uint_as_float((s >> 8) << 23));
             __builtin_nontemporal_store(x.a, kp);
-            __builtin_nontemporal_store(x.b, kp + 1);
+            __builtin_nontemporal_store(x.b, kp + LPR);
             __builtin_nontemporal_store(y.a, vp);
-            __builtin_nontemporal_store(y.b, vp + 1);
+            __builtin_nontemporal_store(y.b, vp + LPR);
         } else {
-            Row16 x, y;
-            x.a = __builtin_nontemporal_load(kp);
-            x.b = __builtin_nontemporal_load(kp + 1);
-            y.a = __builtin_nontemporal_load(vp);
-            y.b = __builtin_nontemporal_load(vp + 1);
+            const Row16 x = {kp[0], kp[LPR]}, y = {vp[0], vp[LPR]};
             unsigned ks, vs;
-            *kc = quantise<D>(x, &ks);
-            *vc = quantise<D>(y, &vs);
+            const u32x4 k = quantise<D>(x, &ks), v = quantise<D>(y, &vs);
+            __builtin_nontemporal_store(u32x2{k[0], k[1]}, kc);
+            __builtin_nontemporal_store(u32x2{k[2], k[3]}, kc + LPR);
+            __builtin_nontemporal_store(u32x2{v[0], v[1]}, vc);
+            __builtin_nontemporal_store(u32x2{v[2], v[3]}, vc + LPR);
             if (c == 0) *sc = (uint16_t)(ks | vs << 8);
         }
     }
