@@ -128,7 +128,7 @@ int64_t pbkv_page_bytes(const pbkv_shape *shape);
  *   out                                   : device, written; rows of other calls untouched
  * With an 8-bit pool the prefix is the values that the pool holds; the suffix, k_new and v_new, is not quantised.  Q is not rounded then
  * (with a bf16 pool once more, after its scaling).
- * bf16: fp32 accumulation, probabilities rounded to bf16 before the PV product, one
+ * bf16 and 8-bit pools: fp32 accumulation, probabilities rounded to bf16 before the PV product, one
  * final rounding to bf16.  f32: fp32 throughout.
  * A call repeated on the same inputs gives the same bits (unless memory for partial results runs out in
  * between).  A launch that would leave CUs idle is split over
@@ -200,7 +200,7 @@ int pbkv_swap_in_pages(const pbkv_shape *shape, const void *host_pages,
  * token is expected to be in the pool already (append first).  context_lens[r] == 0 gives a zero row.
  *   q, out      : device, [batch][H_q][d], bf16 (PBKV_F32: PBKV_ERR_DTYPE)
  *   kv_pool, block_table : device, read only;   context_lens : host int32 [batch]
- * fp32 accumulation, probabilities kept in fp32, one final rounding to bf16.  The library keeps,
+ * fp32 accumulation, probabilities kept in fp32 (over an 8-bit pool as two bf16 numbers, 16 bits), one final rounding to bf16.  The library keeps,
  * per stream, a device scratch buffer for the partial results of context slices (8 MiB on first
  * use; a call that needs more drains that stream and re-allocates); calls on different streams
  * use different buffers and may overlap.
@@ -243,7 +243,7 @@ int pbkv_swap_out_pages(const pbkv_shape *shape, const void *kv_pool, const int3
 
 /*
  * Gather diagnostic (measurement aid, not a step of the method): runs the page gather of
- * pbkv_prefix_prefill on bf16 inputs -- the work units of an unsplit launch (in the forced shape,
+ * pbkv_prefix_prefill on bf16 inputs and pools (others: PBKV_ERR_DTYPE) -- the work units of an unsplit launch (in the forced shape,
  * or the one the library chooses before it decides on splitting a launch over the context), the
  * same walk through block_table, the same loads of K/V rows into on-chip memory -- without the
  * arithmetic,

@@ -53,6 +53,15 @@
 // of each suffice while K(j+1) and V(j) are in flight.  The reference M is moved (and O
 // rescaled, one iteration later, once the product formed under the old M has been added)
 // only when a row maximum exceeds it by more than 2^8.
+//
+// 8-bit pools (KV8).  The same kernels; the pool's rows come as e4m3 codes with a power-of-two scale each, which are bf16 numbers, so a tile in LDS is
+// what a bf16 pool's would be (struct Codes).  What differs:
+//   * codes pass through registers: asked for a step ahead, converted (two per instruction, the scale with them) and stored to LDS between the
+//     MFMAs of a step.  Half the bytes come from the pool; a step has 40 instructions more (of 450).
+//   * Q is not scaled and rounded a second time: scores are exact products, and scale and reference are one FMA in front of each exponential (2.3e-3
+//     from the exact result instead of 2.9e-3).  Q rounded and the reference in the accumulator would save 32 FMAs of a step (64 in the 64-row form).
+// us, over an 8-bit and over a bf16 pool: 12001 + 37 tokens, 32/8 heads of 128, 24.0 and 20.7 (latency of a step's codes: load, convert, store, barrier, read);
+// 4 x 512 behind 2048 shared 78.4 and 73; 2 x 2048 behind 32768 1808 and 1690 (1.25 PFLOP/s); 16/2 heads of 64, 6 of 100 .. 2000 behind up to 1500 39.2 and 34.5.
 #include "pbkv_internal.h"
 
 #include <algorithm>
@@ -180,6 +189,9 @@ int attn_bf16_tile_tokens(int /*head_dim*/, int group, int waves) {
 // and go to LDS as the bf16 numbers that they stand for, in the places that the direct loads of bf16 rows fill.  The tile then is what
 // a bf16 pool's would be, and nothing behind it knows the difference.  A code is converted once per work-group, by one instruction for two,
 // its scale with it.  Lanes of rows past the prefix's end read nothing and write zeros.
+// A lane's 16 codes are two chunks of LDS, so a store writes every other chunk of a row and takes twice its time (7 to 11 % of a launch's LDS clocks).  Lanes
+// in an order in which no two meet in a bank cost more at the loads, whose lines they take in pieces: 24.0 -> 25.3, 78.4 -> 79.5 and 1808 -> 1832 us
+// (launches as above; the narrow-head one 39.2 -> 39.1).
 template <int D, int NW>
 struct Codes {
     using Gm = Geom<D, NW>;
@@ -1183,8 +1195,8 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
     const int n_prefix_pages = (td.prefix_len + 15) >> 4;
     // A wave alone on its SIMD pays for every scalar instruction, so the page ids are held as page
     // offsets in units of 256 bytes (a page is a multiple of that, and a pool of less than 1 TiB
-    // keeps them in 32 bits; the host checks it; an 8-bit page is one of 128, its pool less than half as large): a tile's K address is one lane read, one shift and
-    // one 64-bit add.
+    // keeps them in 32 bits; the host checks it), or of 128 for 8-bit pages, whose pools are half as large:
+    // a tile's K address is one lane read, one shift and one 64-bit add.
     constexpr int UNIT = KV8 ? 7 : 8;
     const int row_pitch = p.Hkv * ROWB;
     const int64_t page_bytes = KV8 ? kv8_page_bytes(p.Hkv, D) : 2 * (int64_t)p.Hkv * 16 * ROWB;
