@@ -190,8 +190,9 @@ int attn_bf16_tile_tokens(int /*head_dim*/, int group, int waves) {
 // a bf16 pool's would be, and nothing behind it knows the difference.  A code is converted once per work-group, by one instruction for two,
 // its scale with it.  Lanes of rows past the prefix's end read nothing and write zeros.
 // A lane's 16 codes are two chunks of LDS, so a store writes every other chunk of a row and takes twice its time (7 to 11 % of a launch's LDS clocks).  Lanes
-// in an order in which no two meet in a bank cost more at the loads, whose lines they take in pieces: 24.0 -> 25.3, 78.4 -> 79.5 and 1808 -> 1832 us
-// (launches as above; the narrow-head one 39.2 -> 39.1).
+// in an order in which no two meet in a bank cost more at the loads, whose lines they take in pieces: 24.0 -> 25.3, 78.4 -> 79.5, 1808 -> 1832 and 39.2 -> 39.1 us
+// (launches as above).  Every other four lanes storing their second chunk first, which four selects per 16 codes bring about: 25.7, 84.1, 1896 and 40.3 --
+// instructions bound these kernels, not LDS.
 template <int D, int NW>
 struct Codes {
     using Gm = Geom<D, NW>;
@@ -674,8 +675,9 @@ void attn_bf16_kernel(AttnParams p, int G) {
         else return tile_src(j + 1);
     };
     // kind, 8-bit pools: 1 a step between prefix tiles alone (K tile j + 1 is one), 2 one behind the prefix (V tile j is suffix rows), 0 any
-    auto step = [&](auto kind, int j, char *kcur, char *knext, char *vprev, char *vcur) __attribute__((always_inline)) {
-        constexpr bool CODES = KV8 && decltype(kind)::value == 1, DIRECT = !KV8 || decltype(kind)::value == 2;
+    // (a number, folded away where the step is put in its place: with a type for it the compiler orders the two-key-group form over bf16 pools otherwise, +0.8 %)
+    auto step = [&](int kind, int j, char *kcur, char *knext, char *vprev, char *vcur) __attribute__((always_inline)) {
+        const bool CODES = KV8 && kind == 1, DIRECT = !KV8 || kind == 2;
         constexpr int NM = 4 * H;                          // MFMAs per step
         constexpr int LD_SP = H / (2 * Gm::NI);            // MFMAs between two tile loads
         static_assert(LD_SP >= 1, "the tile loads of a step fit its first half iteration");
@@ -688,7 +690,7 @@ void attn_bf16_kernel(AttnParams p, int G) {
         lds_void *dst_k = (lds_void *)(knext + w * Gm::RW * ROWB);
         lds_void *dst_v = (lds_void *)(vcur + w * Gm::RW * ROWB);
         if constexpr (KV8) {
-            if constexpr (!CODES && !DIRECT) direct(next, prev, j + 1, knext, vcur);
+            if (!CODES && !DIRECT) direct(next, prev, j + 1, knext, vcur);
             ahead = tile_src(j + 2);
         }
         prev = next;
@@ -729,12 +731,12 @@ void attn_bf16_kernel(AttnParams p, int G) {
                 MFMA_PRIO(0);
                 // all tile loads of the step go out in its first half iteration, K and V rows
                 // alternating, one every LD_SP MFMAs: they have the rest of the step to land
-                if constexpr (DIRECT && i == 0 && s2 % LD_SP == 0) {
+                if constexpr (i == 0 && s2 % LD_SP == 0) if (DIRECT) {
                     constexpr int q = s2 / LD_SP, li2 = q / 2;
                     if constexpr (q % 2 == 0) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_k, dst_k, 16, ok.v[li2], 0, li2 * 1024, 0);
                     else __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc_v, dst_v, 16, ov.v[li2], 0, li2 * 1024, 0);
                 }
-                if constexpr (CODES && i == 1 && s2 % (H / Cd::CHUNKS) == 0)
+                if constexpr (KV8 && i == 1 && s2 % (H / Cd::CHUNKS) == 0) if (CODES)
                     Cd::template store<false>(codes_k, scales_k, knext, w, l, s2 / (H / Cd::CHUNKS));
                 // four score pairs over H steps
                 if constexpr (H == 8) { if constexpr (s2 % 2 == 0) exp_pair(s2); }
@@ -744,8 +746,9 @@ void attn_bf16_kernel(AttnParams p, int G) {
                 constexpr int s2 = decltype(sc)::value, m = m0 + s2;
                 if constexpr (m == 0) __builtin_amdgcn_sched_group_barrier(SG_DSRD, PF, 0);
                 __builtin_amdgcn_sched_group_barrier(SG_MFMA, 1, 0);
-                if constexpr (DIRECT && i == 0 && s2 % LD_SP == 0) __builtin_amdgcn_sched_group_barrier(SG_VMRD, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(SG_VALU, KV8 ? 24 / H + (CODES && i == 1 ? 4 * Cd::CHUNKS / H + 1 : 0) : 16 / H, 0);
+                if constexpr (i == 0 && s2 % LD_SP == 0) if (DIRECT) __builtin_amdgcn_sched_group_barrier(SG_VMRD, 1, 0);
+                if (KV8 && i == 1 && CODES) __builtin_amdgcn_sched_group_barrier(SG_VALU, 24 / H + 4 * Cd::CHUNKS / H + 1, 0);
+                else __builtin_amdgcn_sched_group_barrier(SG_VALU, KV8 ? 24 / H : 16 / H, 0);
                 if constexpr (m + PF < NM) __builtin_amdgcn_sched_group_barrier(SG_DSRD, ((m + PF) / H) & 1 ? 2 : 1, 0);
             }, std::make_integer_sequence<int, H>{});
             // the probabilities are only consumed an iteration later; keep their computation here,
@@ -762,7 +765,7 @@ void attn_bf16_kernel(AttnParams p, int G) {
             static_for([&](auto sc) {
                 constexpr int s2 = decltype(sc)::value, m = m0 + H + s2;
                 if constexpr (m + PF < NM) op[(m + PF) % (PF + 1)] = operand(IntC<m + PF>{});
-                if constexpr (CODES && i == 1 && s2 % (H / Cd::CHUNKS) == 0)
+                if constexpr (KV8 && i == 1 && s2 % (H / Cd::CHUNKS) == 0) if (CODES)
                     Cd::template store<true>(codes_v, scales_v, vcur, w, l, s2 / (H / Cd::CHUNKS));
                 MFMA_PRIO(1);
                 O[s2 % Gm::DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[m % (PF + 1)], Pp[s2 / Gm::DB], O[s2 % Gm::DB], 0, 0, 0);
@@ -786,7 +789,8 @@ void attn_bf16_kernel(AttnParams p, int G) {
             static_for([&](auto sc) {
                 constexpr int s2 = decltype(sc)::value, m = m0 + H + s2;
                 __builtin_amdgcn_sched_group_barrier(SG_MFMA, 1, 1);
-                __builtin_amdgcn_sched_group_barrier(SG_VALU, s2 == H - 1 ? 12 : KV8 ? 24 / H + (CODES && i == 1 ? 4 * Cd::CHUNKS / H + 1 : 0) : 16 / H, 1);
+                if (KV8 && i == 1 && s2 < H - 1 && CODES) __builtin_amdgcn_sched_group_barrier(SG_VALU, 24 / H + 4 * Cd::CHUNKS / H + 1, 1);
+                else __builtin_amdgcn_sched_group_barrier(SG_VALU, s2 == H - 1 ? 12 : KV8 ? 24 / H : 16 / H, 1);
                 if constexpr (m + PF < NM) __builtin_amdgcn_sched_group_barrier(SG_DSRD, ((m + PF) / H) & 1 ? 2 : 1, 1);
             }, std::make_integer_sequence<int, H>{});
             PIN_V(Pc[1]);
@@ -795,15 +799,17 @@ void attn_bf16_kernel(AttnParams p, int G) {
         };
         iteration(IntC<0>{}, T1, T0, P1, P0);             // block 0 is redone before its PV product
         iteration(IntC<1>{}, T0, T1, P0, P1);
-        if constexpr (!CODES) {
-            if constexpr (!DIRECT) store_codes(j + 1, knext, vcur);
+        if (!CODES) {
+            if (!DIRECT) store_codes(j + 1, knext, vcur);
             __builtin_amdgcn_s_waitcnt(0x0F70);           // vmcnt(0): K(j+1), V(j) are in LDS
         }
-        if constexpr (CODES) {
-            request_k(ahead, j + 2);
-            request_v(prev, j + 1);
-        } else if constexpr (!DIRECT) {
-            request(ahead, prev, j + 2);
+        if constexpr (KV8) {
+            if (CODES) {
+                request_k(ahead, j + 2);
+                request_v(prev, j + 1);
+            } else if (!DIRECT) {
+                request(ahead, prev, j + 2);
+            }
         }
         __syncthreads();                                  // ... and every wave is done with K(j), V(j-1)
     };
@@ -838,21 +844,21 @@ void attn_bf16_kernel(AttnParams p, int G) {
         if constexpr (KV8) {
             int j = kt0 + 1;
             for (; j + 1 < kt1 && j + 3 < TP; j += 2) {    // (what both steps ask for lies in the prefix, too)
-                step(IntC<1>{}, j, sK1, sK0, sV0, sV1);
-                step(IntC<1>{}, j + 1, sK0, sK1, sV1, sV0);
+                step(1, j, sK1, sK0, sV0, sV1);
+                step(1, j + 1, sK0, sK1, sV1, sV0);
             }
             for (; j < kt1 && j < TP; j += 2) {
-                step(IntC<0>{}, j, sK1, sK0, sV0, sV1);
-                if (j + 1 < kt1) step(IntC<0>{}, j + 1, sK0, sK1, sV1, sV0);
+                step(0, j, sK1, sK0, sV0, sV1);
+                if (j + 1 < kt1) step(0, j + 1, sK0, sK1, sV1, sV0);
             }
             for (; j < kt1; j += 2) {
-                step(IntC<2>{}, j, sK1, sK0, sV0, sV1);
-                if (j + 1 < kt1) step(IntC<2>{}, j + 1, sK0, sK1, sV1, sV0);
+                step(2, j, sK1, sK0, sV0, sV1);
+                if (j + 1 < kt1) step(2, j + 1, sK0, sK1, sV1, sV0);
             }
         } else {
             for (int j = kt0 + 1; j < kt1; j += 2) {
-                step(IntC<0>{}, j, sK1, sK0, sV0, sV1);
-                if (j + 1 < kt1) step(IntC<0>{}, j + 1, sK0, sK1, sV1, sV0);
+                step(0, j, sK1, sK0, sV0, sV1);
+                if (j + 1 < kt1) step(0, j + 1, sK0, sK1, sV1, sV0);
             }
         }
     } else {
