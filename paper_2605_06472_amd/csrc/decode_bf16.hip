@@ -115,7 +115,7 @@ static __device__ __forceinline__ void merge_slices(const float *base, int64_t s
         for (int w = 0; w < DEC_WAVES; w++) den += red_d[w][h] * weight(red_m[w][h], M);
         bf16x4 r;
 #pragma unroll
-        for (int e = 0; e < 4; e++) r[e] = (__bf16)(den > 0.f ? o[e] / den : 0.f);
+        for (int e = 0; e < 4; e++) r[e] = (__bf16)normalised(o[e], den);
         *(bf16x4 *)(out + it * 4) = r;
     }
 }

@@ -22,6 +22,10 @@ template <int I> struct IntC { static constexpr int value = I; };
 // exp2(m - ref) where m == -inf counts nothing (a wave without pages)
 static __device__ __forceinline__ float weight(float m, float ref) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - ref); }
 
+// A row's value.  The sum of its weights is 0 exactly where nothing counts (no tokens, or scores of -inf alone), and the row zero then; a NaN score
+// makes it NaN in whatever slice it stands (0 * NaN is NaN, however little the slice weighs), and the row's values with it.
+static __device__ __forceinline__ float normalised(float num, float den) { return den == 0.f ? 0.f : num / den; }
+
 // x of this lane and of the lane 32 (16) away, added; lanes whose bit 5 (bit 4) is set get the sum of y instead.
 static __device__ __forceinline__ float fold32(float x, float y) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
@@ -112,7 +116,7 @@ static __device__ __forceinline__ void merge_held(const float *base, int64_t str
         const float den = (red_d[0][ho] + red_d[1][ho]) + (red_d[2][ho] + red_d[3][ho]);
         bf16x4 r;
 #pragma unroll
-        for (int e = 0; e < 4; e++) r[e] = (__bf16)(den > 0.f ? o[e] / den : 0.f);
+        for (int e = 0; e < 4; e++) r[e] = (__bf16)normalised(o[e], den);
         *(bf16x4 *)(out + it * 4) = r;
     };
     f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};      // 512 groups: two per thread; fewer: two chains
