@@ -198,6 +198,7 @@ int pbkv_swap_in_pages(const pbkv_shape *shape, const void *host_pages,
  *     out[r][h] = sum_t softmax_t(q[r][h] . k_t / sqrt(d)) v_t   over t in [0, context_lens[r])
  * with k_t, v_t read from kv_pool through block_table[r] (KV head h / (H_q / H_kv)); the row's own
  * token is expected to be in the pool already (append first).  context_lens[r] == 0 gives a zero row.
+ * A NaN score, or one of plus infinity, makes its row NaN; scores of minus infinity count nothing, and a row that has no others is zero.
  *   q, out      : device, [batch][H_q][d], bf16 (PBKV_F32: PBKV_ERR_DTYPE)
  *   kv_pool, block_table : device, read only;   context_lens : host int32 [batch]
  * fp32 accumulation, probabilities kept in fp32 (over an 8-bit pool as two bf16 numbers, 16 bits), one final rounding to bf16.  The library keeps,

@@ -351,10 +351,10 @@ static __device__ __forceinline__ void decode_slice(const DecodeParams &p, const
             for (int e = 0; e < 4; e++) num[e] = fmaf(f, x[e], num[e]);
             den = fmaf(f, part_l[ww][h], den);
         }
-        if (n_slices == 1) {
+        if (__builtin_expect(n_slices == 1, 1)) {                      // (laid out first: a partial's stores, the wait behind them and the count are one run)
             bf16x4 r;
 #pragma unroll
-            for (int e = 0; e < 4; e++) r[e] = (__bf16)(den > 0.f ? num[e] / den : 0.f);
+            for (int e = 0; e < 4; e++) r[e] = (__bf16)normalised(num[e], den);
             *(bf16x4 *)(out + it * 4) = r;
         } else {
             store_partial<FUSED>(dst + it * 4, num[0], num[1]);
