@@ -1043,9 +1043,9 @@ void attn_bf16_kernel(AttnParams p, int G) {
 // the classes given by hand: the output accumulators O live in accumulation registers (only MFMAs
 // touch them on the common path), the scores, probabilities, references and Q operands in vector
 // registers.  Assembly statements get no hazard handling from the compiler; the pipeline keeps
-// every producer at least a half iteration (16 MFMAs) ahead of its consumer, and the three places
-// where that is not so (masking right after a score chain, the rare reference move, the epilogue)
-// wait explicitly.
+// every producer at least a half iteration (16 MFMAs) ahead of its consumer, and the four places
+// where that is not so (masking right after a score chain, the rare reference move, the end of a loop, the
+// epilogue) wait explicitly.  The tests look for the waits along every path of the assembly.
 // A wave alone on its SIMD issues in order with nothing to cover for it, so the place of every
 // instruction counts: the exponentials and packs of the common path are assembly statements too
 // (plain intrinsics carry no ordering against the MFMA statements and were all gathered in front
@@ -1060,6 +1060,10 @@ typedef __attribute__((ext_vector_type(4))) int i32x4;
 // d = a b + c, scores: everything in vector registers except the Q operand b
 static __device__ __forceinline__ void mfma_s_first(f32x16 &d, const i32x4 &a, const i32x4 &b, const f32x16 &c) {
     asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %3" : "=&v"(d) : "v"(a), "v"(b), "v"(c));
+}
+// ... + 0, as a constant: a register written right before would not be there yet (two wait states, which no one puts in for a statement)
+static __device__ __forceinline__ void mfma_s_zero(f32x16 &d, const i32x4 &a, const i32x4 &b) {
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(d) : "v"(a), "v"(b));
 }
 static __device__ __forceinline__ void mfma_s_acc(f32x16 &d, const i32x4 &a, const i32x4 &b) {
     asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(d) : "v"(a), "v"(b));
@@ -1184,9 +1188,9 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
 #pragma unroll
             for (int dc = 0; dc < Gm::DC; dc++) asm volatile("" : "+a"(qreg[s][dc]));
     }
-    auto s_first = [](f32x16 &d, const i32x4 &a, const i32x4 &b, const f32x16 &c) __attribute__((always_inline)) {
+    auto s_zero = [](f32x16 &d, const i32x4 &a, const i32x4 &b) __attribute__((always_inline)) {
         if constexpr (KV8) mfma_s_first_q(d, a, b);
-        else mfma_s_first(d, a, b, c);
+        else mfma_s_zero(d, a, b);
     };
     auto s_acc = [](f32x16 &d, const i32x4 &a, const i32x4 &b) __attribute__((always_inline)) {
         if constexpr (KV8) mfma_s_acc_q(d, a, b);
@@ -1556,13 +1560,13 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
                     put_bits(bits, Pc[0], 2 * PPG * s2);
                 } else {
                 f32x2 pv[PPG];
-                if constexpr (s2 == 0) s_first(Tn[0], op[m % (PFW + 1)], qreg[0][s2], negM[0]);
-                else s_acc(Tn[0], op[m % (PFW + 1)], qreg[0][s2]);
+                if constexpr (s2 == 0) mfma_s_first(Tn[0], op[m % (PFW + 1)], qreg[0][s2], negM[0]);
+                else mfma_s_acc(Tn[0], op[m % (PFW + 1)], qreg[0][s2]);
                 __builtin_amdgcn_sched_barrier(0);
                 static_for([&](auto pc) { pv[pc.value] = exp_pair_a(Tc[0], 2 * (PPG * s2 + pc.value)); }, std::make_integer_sequence<int, PPG>{});
                 __builtin_amdgcn_sched_barrier(0);
-                if constexpr (s2 == 0) s_first(Tn[1], op[m % (PFW + 1)], qreg[1][s2], negM[1]);
-                else s_acc(Tn[1], op[m % (PFW + 1)], qreg[1][s2]);
+                if constexpr (s2 == 0) mfma_s_first(Tn[1], op[m % (PFW + 1)], qreg[1][s2], negM[1]);
+                else mfma_s_acc(Tn[1], op[m % (PFW + 1)], qreg[1][s2]);
                 __builtin_amdgcn_sched_barrier(0);
                 if constexpr (!KV8 && i == 0 && s2 < NL) {
                     constexpr int li2 = s2 / 2;
@@ -1633,10 +1637,10 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
         static_for([&](auto dc) {
             const i32x4 a0 = k_operand(sK0, 0, dc.value), a1 = k_operand(sK0, 1, dc.value);
             if constexpr (dc.value == 0) {
-                s_first(T0[0], a0, qreg[0][0], negM[0]);
-                s_first(T0[1], a0, qreg[1][0], negM[1]);
-                s_first(T1[0], a1, qreg[0][0], negM[0]);
-                s_first(T1[1], a1, qreg[1][0], negM[1]);
+                s_zero(T0[0], a0, qreg[0][0]);             // (the reference is 0)
+                s_zero(T0[1], a0, qreg[1][0]);
+                s_zero(T1[0], a1, qreg[0][0]);
+                s_zero(T1[1], a1, qreg[1][0]);
             } else {
                 s_acc(T0[0], a0, qreg[0][dc.value]);
                 s_acc(T0[1], a0, qreg[1][dc.value]);
@@ -1659,21 +1663,27 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
         __syncthreads();
         static_for([&](auto mc) { op[mc.value] = k_operand(sK1, 0, mc.value); }, std::make_integer_sequence<int, PFW>{});
     }
+    // Behind a loop O may go on in other registers, to which it is moved once the last products are there.
+    auto settle_outputs = [&]() __attribute__((always_inline)) {
+        if constexpr (D == 128)
+            asm volatile("s_nop 15\n\ts_nop 3" : "+a"(O[0][0]), "+a"(O[0][1]), "+a"(O[0][2]), "+a"(O[0][3]), "+a"(O[1][0]), "+a"(O[1][1]), "+a"(O[1][2]), "+a"(O[1][3]));
+        else
+            asm volatile("s_nop 15\n\ts_nop 3" : "+a"(O[0][0]), "+a"(O[0][1]), "+a"(O[1][0]), "+a"(O[1][1]));
+    };
     int first = 1;
     if constexpr (KV8) {
         for (; first + 3 < TP; first += 2) {               // (what both steps ask for lies in the prefix, too)
             step(IntC<1>{}, first, sK1, sK0, sV0, sV1);
             step(IntC<1>{}, first + 1, sK0, sK1, sV1, sV0);
         }
-        // the other loop holds O in other registers: it is moved once the last products are there
-        if constexpr (D == 128)
-            asm volatile("s_nop 15\n\ts_nop 3" : "+a"(O[0][0]), "+a"(O[0][1]), "+a"(O[0][2]), "+a"(O[0][3]), "+a"(O[1][0]), "+a"(O[1][1]), "+a"(O[1][2]), "+a"(O[1][3]));
-        else
-            asm volatile("s_nop 15\n\ts_nop 3" : "+a"(O[0][0]), "+a"(O[0][1]), "+a"(O[1][0]), "+a"(O[1][1]));
+        settle_outputs();
     }
-    for (int j = first; j < n_tiles; j += 2) {
-        step(IntC<0>{}, j, sK1, sK0, sV0, sV1);
-        if (j + 1 < n_tiles) step(IntC<0>{}, j + 1, sK0, sK1, sV1, sV0);
+    if (first < n_tiles) {
+        for (int j = first; j < n_tiles; j += 2) {
+            step(IntC<0>{}, j, sK1, sK0, sV0, sV1);
+            if (j + 1 < n_tiles) step(IntC<0>{}, j + 1, sK0, sK1, sV1, sV0);
+        }
+        if constexpr (!KV8) settle_outputs();
     }
     // drain: probabilities of the last block, products of tile n_tiles - 1
     {
