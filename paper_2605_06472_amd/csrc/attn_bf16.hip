@@ -1319,8 +1319,9 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
     for (int s = 0; s < 2; s++)
 #pragma unroll
         for (int r = 0; r < 16; r++) negM[s][r] = 0.f;
-    // (8-bit pools: the reference, and the largest row sum of a block that leaves it where it is; see the kernel above)
-    [[maybe_unused]] float ref[2] = {0.f, 0.f}, lb_max[2] = {-1.f, -1.f};
+    // (the largest row sum of a block that leaves the reference where it is, and for 8-bit pools the reference; see the kernel above)
+    float lb_max[2] = {-1.f, -1.f};
+    [[maybe_unused]] float ref[2] = {0.f, 0.f};
 
     int k_off[Gm::DC];
 #pragma unroll
@@ -1442,22 +1443,18 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
             }
         }
     };
-    auto line = [&](int s) __attribute__((always_inline)) { return KV8 ? lb_max[s] : RESCALE_SUM; };
     // the reference move of one sub-tile (see the kernel above); its scores and outputs have settled
-    auto redo_block = [&](int s, f32x16 &Tc, f32x16 &Tn, bf16x8 (&Pp)[2], bool first_check) __attribute__((always_inline)) {
+    auto redo_block = [&](int s, f32x16 &Tc, f32x16 &Tn, bf16x8 (&Pp)[2]) __attribute__((always_inline)) {
         float mxp = Tn[0];
 #pragma unroll
         for (int r = 1; r < 16; r++) mxp = fmaxf(mxp, Tn[r]);
         mxp = xmax32(mxp);
-        bool first = first_check, none = false;
-        if constexpr (KV8) {
-            mxp = fmaf(mxp, c, -ref[s]);
-            first = xsum32(l_part[s]) == 0.f;                     // nothing of this row has counted so far
-            none = first && mxp == -INFINITY;
-            lb_max[s] = __any(none) ? -1.f : RESCALE_SUM;
-        }
+        if constexpr (KV8) mxp = fmaf(mxp, c, -ref[s]);
+        const bool first = xsum32(l_part[s]) == 0.f;              // nothing of this row has counted so far
+        const bool none = first && mxp == -INFINITY;
         const float d = none ? 0.f : first ? mxp : fmaxf(mxp, 0.f);
         const float alpha = first ? 1.f : __builtin_amdgcn_exp2f(-d);
+        lb_max[s] = __any(none) ? -1.f : RESCALE_SUM;
         l_part[s] *= alpha;
 #pragma unroll
         for (int db = 0; db < Gm::DB; db++) O[s][db] *= alpha;
@@ -1472,15 +1469,15 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
 #pragma unroll
         for (int r = 0; r < 16; r += 2) exp_pair(s, Tn, Pp, lb[s], r);
     };
-    auto redo_both = [&](f32x16 (&Tc)[2], f32x16 (&Tn)[2], bf16x8 (&Pp)[2][2], bool first_check) __attribute__((always_inline)) {
+    auto redo_both = [&](f32x16 (&Tc)[2], f32x16 (&Tn)[2], bf16x8 (&Pp)[2][2]) __attribute__((always_inline)) {
         SETTLE_V2(Tn[0], Tn[1]);
         SETTLE_V2(Tc[0], Tc[1]);
 #pragma unroll
         for (int db = 0; db < Gm::DB; db++) SETTLE_A2(O[0][db], O[1][db]);
         // each sub-tile moves its reference exactly when a wave serving it alone would
-        const bool r0 = __any(!(lb[0] <= line(0))), r1 = __any(!(lb[1] <= line(1)));
-        if ((!KV8 && first_check) || r0) redo_block(0, Tc[0], Tn[0], Pp[0], first_check);
-        if ((!KV8 && first_check) || r1) redo_block(1, Tc[1], Tn[1], Pp[1], first_check);
+        const bool r0 = __any(!(lb[0] <= lb_max[0])), r1 = __any(!(lb[1] <= lb_max[1]));
+        if (r0) redo_block(0, Tc[0], Tn[0], Pp[0]);
+        if (r1) redo_block(1, Tc[1], Tn[1], Pp[1]);
         if constexpr (!KV8) SETTLE_V2(negM[0], negM[1]);
 #pragma unroll
         for (int db = 0; db < Gm::DB; db++) SETTLE_A2(O[0][db], O[1][db]);
@@ -1536,12 +1533,12 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
             op[(m + PFW) % (PFW + 1)] = operand(IntC<m + PFW>{});
         };
 
-        auto iteration = [&](auto ic, f32x16 (&Tc)[2], f32x16 (&Tn)[2], bf16x8 (&Pc)[2][2], bf16x8 (&Pp)[2][2], bool first_check) __attribute__((always_inline)) {
+        auto iteration = [&](auto ic, f32x16 (&Tc)[2], f32x16 (&Tn)[2], bf16x8 (&Pc)[2][2], bf16x8 (&Pp)[2][2]) __attribute__((always_inline)) {
             constexpr int i = decltype(ic)::value;
             constexpr int m0 = i * 2 * H;
             constexpr int PPG = 8 / H;                     // score pairs exponentiated beside one operand's two MFMAs
             block_sums(Pp);
-            if (__builtin_expect((!KV8 && first_check) || __any(!(lb[0] <= line(0)) || !(lb[1] <= line(1))), 0)) redo_both(Tc, Tn, Pp, first_check);
+            if (__builtin_expect(__any(!(lb[0] <= lb_max[0]) || !(lb[1] <= lb_max[1])), 0)) redo_both(Tc, Tn, Pp);
             l_part[0] += lb[0];
             l_part[1] += lb[1];
             lb[0] = 0.f;
@@ -1619,8 +1616,8 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
                 __builtin_amdgcn_sched_barrier(0);
             }, std::make_integer_sequence<int, H>{});
         };
-        iteration(IntC<0>{}, T1, T0, P1, P0, j == 1);
-        iteration(IntC<1>{}, T0, T1, P0, P1, false);
+        iteration(IntC<0>{}, T1, T0, P1, P0);
+        iteration(IntC<1>{}, T0, T1, P0, P1);
     };
     // fill: scores of tile 0 for both sub-tiles; K(1), V(0) fetched
     {
@@ -1701,7 +1698,7 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
             }, std::make_integer_sequence<int, H>{});
         };
         block_sums(P0);
-        if ((!KV8 && n_tiles == 1) || __any(!(lb[0] <= line(0)) || !(lb[1] <= line(1)))) redo_both(T1, T0, P0, n_tiles == 1);
+        if (__any(!(lb[0] <= lb_max[0]) || !(lb[1] <= lb_max[1]))) redo_both(T1, T0, P0);
         l_part[0] += lb[0];
         l_part[1] += lb[1];
         lb[0] = 0.f;
@@ -1710,7 +1707,7 @@ void attn_bf16_w64_kernel(AttnParams p, int G) {
         exp_all(0, T1[0], P1[0]);
         exp_all(1, T1[1], P1[1]);
         product(0, P0);
-        if (__any(!(lb[0] <= line(0)) || !(lb[1] <= line(1)))) redo_both(T0, T1, P1, false);
+        if (__any(!(lb[0] <= lb_max[0]) || !(lb[1] <= lb_max[1]))) redo_both(T0, T1, P1);
         l_part[0] += lb[0];
         l_part[1] += lb[1];
         product(1, P1);
