@@ -106,6 +106,8 @@ typedef struct {
  * Scale bytes have to be in 16 .. 246, as append leaves them, in every slot that a call reads as a token.  Other slots may hold
  * anything.  A row with a NaN makes the results that depend on it NaN.  In all calls the same limits hold as for PBKV_BF16, but for the
  * pool's size, which is less than 512 GiB, and a page's, less than 2 GiB.
+ * What attention forms on the way has to be in fp32's range, or it is infinite: over any pool the sums of weights, up to 2^8 each, times values, before
+ * the division by the weights' sum; over an 8-bit pool q . k before its division by sqrt(d), and in decode q . code before the row's scale (it is for |q| up to 2^112).
  */
 
 /* Bytes of one pool page for this shape: 2 * H_kv * P * d * element size, or 2 * H_kv * P * (d + 1) rounded up to a multiple of 128
@@ -201,7 +203,8 @@ int pbkv_swap_in_pages(const pbkv_shape *shape, const void *host_pages,
  * A NaN score, or one of plus infinity, makes its row NaN; scores of minus infinity count nothing, and a row that has no others is zero.
  *   q, out      : device, [batch][H_q][d], bf16 (PBKV_F32: PBKV_ERR_DTYPE)
  *   kv_pool, block_table : device, read only;   context_lens : host int32 [batch]
- * fp32 accumulation, probabilities kept in fp32 (over an 8-bit pool as two bf16 numbers, 16 bits), one final rounding to bf16.  The library keeps,
+ * fp32 accumulation, probabilities kept in fp32 (over an 8-bit pool, times the row's scale, as two bf16 numbers: off by 2^-17 of it, or by
+ * 2^-134 where that is more), one final rounding to bf16.  The library keeps,
  * per stream, a device scratch buffer for the partial results of context slices (8 MiB on first
  * use; a call that needs more drains that stream and re-allocates); calls on different streams
  * use different buffers and may overlap.

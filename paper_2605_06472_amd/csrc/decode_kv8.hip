@@ -10,8 +10,8 @@
 //              being loaded in the same order.  Codes become bf16 exactly, two per instruction, without their scale: that
 //              multiplies the token's score, of which a lane has four, and not its 8 d.
 //   P V        on the 16x16x16 bf16 MFMA, which takes the page's 16 tokens at once: V codes are bf16 numbers, and a probability (times its
-//              token's scale) goes in as two, the nearest and what that leaves, 16 bits in all -- an error of 2^-17 of it, where the result
-//              is rounded to 2^-8.  Against the bf16 kernel's fp32 forms that is as fast up to 4 heads (201 us both for 64 requests of 1024 ..
+//              token's scale) goes in as two, the nearest and what that leaves, 16 bits in all -- an error of 2^-17 of it (at scales near 2^-111 half of
+//              bf16's smallest step, 2^-134, where that is more), where the result is rounded to 2^-8.  Against the bf16 kernel's fp32 forms that is as fast up to 4 heads (201 us both for 64 requests of 1024 ..
 //              16384 tokens at 32/8 heads of 128), whose 4x4x1 products take as many clocks, and faster past it: 62.4 -> 58.1 at 16/2, 80.4 -> 62.9 at
 //              32/2, 36.0 -> 32.3 at 16/2 of 64.  A lane holds d E c .. of four tokens, a word each: four by four bytes are transposed, so that a word is
 //              four tokens of one d.  Both scales of its tokens are one 8-byte load.
