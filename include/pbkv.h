@@ -24,7 +24,9 @@
  *     the context (8 MiB on first use, up to 163 MiB where such attention calls need it, more
  *     only where a decode call does; 4 KiB of counters beside it).  All of it is
  *     created on first use and released at process exit.  An attention call for which there is no
- *     memory for partial results runs unsplit; decode then fails with PBKV_ERR_DEVICE.
+ *     memory for partial results runs unsplit; decode then fails with PBKV_ERR_DEVICE.  (Some kernels
+ *     of pbkv_prefix_prefill over 8-bit pools of head_dim 128 use up to 108 bytes a thread of the scratch memory
+ *     that the HIP runtime keeps for each queue; no other attention, decode or copy kernel does.)
  *   - `stream` is a hipStream_t passed as void*; NULL is the default stream.
  *     hipStreamPerThread, one handle on every thread, counts as a stream of its own on each.
  *     Calls validate on the host, enqueue on `stream`, and return without

@@ -60,6 +60,9 @@
 //     MFMAs of a step.  Half the bytes come from the pool; a step has 40 instructions more (of 450).
 //   * Q is not scaled and rounded a second time: scores are exact products, and scale and reference are one FMA in front of each exponential (2.3e-3
 //     from the exact result instead of 2.9e-3).  Q rounded and the reference in the accumulator would save 32 FMAs of a step (64 in the 64-row form).
+//   * the codes' registers come on top: at d = 128 the four-wave forms need more than the 256 there are and keep 68 bytes a thread (two key groups
+//     108) in scratch memory, the only attention, decode or copy kernels with any.  With one key group it is used where references move in mixed steps; with two the
+//     page ids are among it, and their reload, every 16 tiles, makes each step wait for its codes before its first MFMA.
 // us, over an 8-bit and over a bf16 pool: 12001 + 37 tokens, 32/8 heads of 128, 24.0 and 20.7 (latency of a step's codes: load, convert, store, barrier, read);
 // 4 x 512 behind 2048 shared 78.4 and 73; 2 x 2048 behind 32768 1808 and 1690 (1.25 PFLOP/s); 16/2 heads of 64, 6 of 100 .. 2000 behind up to 1500 39.2 and 34.5.
 #include "pbkv_internal.h"

@@ -121,7 +121,7 @@ static __device__ __forceinline__ void decode_kv8_slice(const DecodeParams &p, c
     constexpr int NK = D / 64;             // 16-byte K loads per page, each feeding two MFMAs
     constexpr int E = D / 16;              // d-values of a V row per lane
     constexpr int PR = D + 4;              // floats of a head's row in LDS
-    constexpr int BUFS = 2;                // pages of a wave in registers: one being worked on, the others in flight
+    constexpr int BUFS = 2;                // pages of a wave in registers: one being worked on, the next in flight
     typedef typename CodeRow<D>::type vrow;
 
     const int l = threadIdx.x & 63;
@@ -190,7 +190,7 @@ static __device__ __forceinline__ void decode_kv8_slice(const DecodeParams &p, c
     auto load_page = [&](int k, PageRegs &r) {
         const int64_t at = (int64_t)__builtin_amdgcn_readlane(ids, k & 63) * page_bytes;
         const char *kb = pool_k + at;
-        // codes are read exactly once: streaming loads.  (A line of scales belongs to four KV heads.)
+        // Every byte is read once, but a line of scales belongs to four KV heads and one of K codes to two of these loads: the streaming hint is on V's alone.
         r.s = *(const u32x2 *)(pool_s + at + 8 * g);
 #pragma unroll
         for (int j = 0; j < NK; j++) r.k[j] = *(const u32x4 *)(kb + koff + 64 * j);
@@ -292,7 +292,7 @@ static __device__ __forceinline__ void decode_kv8_slice(const DecodeParams &p, c
         }
     };
 
-    // The next BUFS - 1 pages are in flight while one is being worked on.  Behind the last page it is loaded again (a hit in the caches): where
+    // The next page is in flight while one is being worked on.  Behind the last page that one is loaded again (a hit in the caches): where
     // the load hangs on a condition, the waits for a page's rows have to hold without it too, and wait for the next page's.
     PageRegs rg[BUFS];
     if (n_mine > 0) {

@@ -128,6 +128,8 @@ hipError_t launch_read(const AppendParams &p, int head_dim, int elt_bytes, hipSt
 // saturates the link, and a transfer that runs beside attention or decode (Sec. 4.3: prefetch
 // hidden behind compute) must not park thousands of waves, each waiting microseconds on the
 // link, on the CUs and memory queues the compute kernel needs.
+// Pages of bf16 and fp32 rows are whole parts.  Those of 8-bit rows are not: 33024 bytes (8 heads of 128) are parts of 1024, 1024
+// and 16 chunks, 344 KiB in flight on average, and a page of 4224 bytes (2 of 64) is one of 264; their rates have not been measured.
 constexpr int SWAP_CHUNKS = 1024;   // 16 KiB per work-group and pass
 constexpr int SWAP_MAX_WGS = 32;
 
